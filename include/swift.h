@@ -26,7 +26,8 @@
  * n_layers x [RMSNorm -> rotary (half-split pairs) causal attention with
  * n_q_heads query heads on n_kv_heads key/value heads -> residual add,
  * RMSNorm -> SwiGLU MLP -> residual add], final RMSNorm, untied LM head; no
- * biases.  Weights and the key/value cache are stored in `dtype`; the residual
+ * biases.  Weights and the key/value cache are stored in `dtype` (SWIFT_MXFP4: wq, wk, wv, wo, wg, wu and wd in
+ * 4-bit blocks, see the MXFP4 operators; embedding, LM head and cache in bf16); the residual
  * stream, normalised activations, queries, attention probabilities, MLP
  * intermediates and logits are fp32 and every accumulation is fp32.
  *
@@ -55,6 +56,7 @@ extern "C" {
 
 #define SWIFT_F32 0
 #define SWIFT_BF16 1
+#define SWIFT_MXFP4 2 /* models only: the layers' projections as MXFP4 matrices, everything else as SWIFT_BF16 */
 
 /* Largest number of rows one verify block or token tree may hold (pending token + k drafts): k <=
  * SWIFT_MAX_BLOCK - 1.  The paper's maximum draft length is 25 (Appendix B.2): a chain block of 26 rows. */
@@ -66,7 +68,7 @@ typedef struct swift_model_config {
     int32_t n_layers, hidden, n_q_heads, n_kv_heads, head_dim, ffn, vocab;
     int32_t max_seq;   /* capacity of the key/value cache in tokens */
     float rms_eps, rope_theta;
-    int32_t dtype;     /* SWIFT_F32 or SWIFT_BF16: storage of weights and of the key/value cache */
+    int32_t dtype;     /* SWIFT_F32, SWIFT_BF16 or SWIFT_MXFP4: storage of weights and of the key/value cache */
 } swift_model_config;
 
 /* Counters behind the paper's metrics (Appendix B.3): mean generated length
@@ -120,7 +122,8 @@ int swift_destroy(swift_ctx *ctx);
 
 /* Copies one tensor into the arena, converting to the library's layout.  data: host OR device
  * pointer, row-major [out][in], n_elems elements of type `dtype`, which must equal the model's
- * dtype for matrices and be SWIFT_F32 for the RMSNorm gains.  Names: "embed" [vocab][hidden],
+ * dtype for matrices (SWIFT_MXFP4 models: SWIFT_BF16; the layers' matrices are quantised on the way in, which
+ * changes no value that MXFP4 already represents) and be SWIFT_F32 for the RMSNorm gains.  Names: "embed" [vocab][hidden],
  * "lm_head" [vocab][hidden], "final_norm" [hidden], and for layer i: "l<i>.attn_norm" [hidden],
  * "l<i>.wq" [n_q*d][hidden], "l<i>.wk", "l<i>.wv" [n_kv*d][hidden], "l<i>.wo" [hidden][n_q*d],
  * "l<i>.mlp_norm" [hidden], "l<i>.wg", "l<i>.wu" [ffn][hidden], "l<i>.wd" [hidden][ffn].
@@ -319,6 +322,44 @@ int swift_get_state(swift_ctx *ctx, int *cache_len, int32_t *pending_token);
 /* The configuration the context was created with. */
 int swift_get_config(swift_ctx *ctx, swift_model_config *out);
 int swift_get_stats(swift_ctx *ctx, swift_stats *out);
+
+/* ---- MXFP4 operators -----------------------------------------------------------------------------
+ * Matrices in 4-bit floating point with shared scales (OCP Microscaling Formats v1.0, MXFP4), and the products with them that a model of
+ * dtype SWIFT_MXFP4 is made of, for weights and activations of the caller's own.
+ * A block is 32 consecutive elements of a row (the last one what is left of it) and has a scale 2^e, e = floor(log2(largest magnitude)) - 2,
+ * at least -127; an element is w / 2^e rounded to the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives, ties to the one with
+ * the even code (0, 1, 2, 4), magnitudes above 6 to 6.  A block that holds an infinity or a NaN reads back as NaN throughout.  Quantising what
+ * was read back changes nothing.
+ * All of them: device pointers of the current device, `stream` a hipStream_t (NULL = default stream) on which the work is
+ * enqueued; nothing is allocated, nothing waited for, nothing kept between calls, so that calls may be captured into a graph, and
+ * calls with workspaces of their own may overlap.  Types: SWIFT_F32 or SWIFT_BF16.  Rows may lie apart (ld_*: elements from one
+ * row to the next, at least a row's length) and need no alignment beyond their elements'; packed matrices and workspaces are aligned to 256
+ * bytes.  Outputs must not overlap inputs, except that y may be the residual itself (same pointer and leading dimension).
+ * 1 <= rows, depth <= 2^22.  SWIFT_EINVAL on null pointers, sizes, types and alignments, SWIFT_ECAPACITY on a workspace that is missing
+ * or too small, before anything is enqueued. */
+
+/* Bytes of a packed matrix [rows][depth]; gated != 0: of a gate and an up matrix of `rows` rows each, packed as one. */
+int swift_mx4_bytes(int rows, int depth, int gated, uint64_t *bytes);
+
+/* packed = w [rows][depth] (up != NULL: gate rows w and up rows, [rows][depth] each, as one gated matrix). */
+int swift_mx4_quantize(void *packed, const void *w, int64_t ld_w, const void *up, int64_t ld_up, int dtype, int rows, int depth,
+                       void *stream);
+
+/* w [rows][depth] = the numbers a packed matrix stands for (gated != 0: w [2 * rows][depth], gate rows first), exact in either type. */
+int swift_mx4_dequantize(void *w, int64_t ld_w, int dtype, const void *packed, int rows, int depth, int gated, void *stream);
+
+/* Bytes of workspace that a product of n rows of x_dtype with a packed matrix needs. */
+int swift_mx4_workspace(int rows, int depth, int gated, int n, int x_dtype, uint64_t *bytes);
+
+/* y [n][rows] = x [n][depth] W^T (+ residual [n][rows], of y's type; NULL: none).  Products are exact, sums fp32; y is rounded once.
+ * n = 0 does nothing.  A row with an infinity or a NaN leaves the others as they are. */
+int swift_mx4_linear(void *y, int64_t ld_y, int y_dtype, const void *x, int64_t ld_x, int x_dtype, int n, const void *packed, int rows,
+                     int depth, const void *residual, int64_t ld_residual, void *workspace, uint64_t workspace_bytes, void *stream);
+
+/* h [n][rows] = silu(x Wg^T) * (x Wu^T), silu(v) = v / (1 + exp(-v)), of a gated packed matrix: the first half of a gated feed-forward
+ * block in one product. */
+int swift_mx4_swiglu(void *h, int64_t ld_h, int h_dtype, const void *x, int64_t ld_x, int x_dtype, int n, const void *packed, int rows,
+                     int depth, void *workspace, uint64_t workspace_bytes, void *stream);
 
 /* ---- test and measurement hooks -------------------------------------------------------------- */
 

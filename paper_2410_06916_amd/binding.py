@@ -12,7 +12,8 @@ import numpy as np
 
 from . import build as _build
 
-F32, BF16 = 0, 1
+F32, BF16, MXFP4 = 0, 1, 2
+_MODEL_DTYPES = {"fp32": F32, "bf16": BF16, "mxfp4": MXFP4}
 MAX_BLOCK = 32
 MAX_WINDOW = 128   # longest candidate-evaluation window (SWIFT_MAX_WINDOW)
 TOPK = 10
@@ -110,6 +111,13 @@ def lib():
     L.swift_debug_attn_path.argtypes = [vp, C.c_int, C.c_int, C.c_char_p, C.c_int]
     L.swift_debug_projection_path.argtypes = [C.POINTER(ModelConfig), C.c_int, C.c_int, C.c_int, C.c_int, C.c_char_p, C.c_int]
     L.swift_debug_prompt_path.argtypes = [C.POINTER(ModelConfig), C.c_int, C.c_int, C.c_int, C.c_int, C.c_char_p, C.c_int]
+    i64 = C.c_int64
+    L.swift_mx4_bytes.argtypes = [C.c_int, C.c_int, C.c_int, C.POINTER(C.c_uint64)]
+    L.swift_mx4_workspace.argtypes = [C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_uint64)]
+    L.swift_mx4_quantize.argtypes = [vp, vp, i64, vp, i64, C.c_int, C.c_int, C.c_int, vp]
+    L.swift_mx4_dequantize.argtypes = [vp, i64, C.c_int, vp, C.c_int, C.c_int, C.c_int, vp]
+    L.swift_mx4_linear.argtypes = [vp, i64, C.c_int, vp, i64, C.c_int, C.c_int, vp, C.c_int, C.c_int, vp, i64, vp, C.c_uint64, vp]
+    L.swift_mx4_swiglu.argtypes = [vp, i64, C.c_int, vp, i64, C.c_int, C.c_int, vp, C.c_int, C.c_int, vp, C.c_uint64, vp]
     L.swift_profile_class.argtypes = [vp, C.c_int]
     L.swift_profile_read.argtypes = [vp, C.POINTER(C.c_int64), C.POINTER(C.c_double), C.POINTER(C.c_uint64)]
     _lib = L
@@ -127,9 +135,9 @@ def _p(a: np.ndarray, ty):
 
 def make_config(shape, max_seq: int) -> ModelConfig:
     """shape: any object with n_layers, hidden, n_q_heads, n_kv_heads, head_dim, ffn, vocab,
-    rms_eps, rope_theta, dtype ("fp32" | "bf16")."""
+    rms_eps, rope_theta, dtype ("fp32" | "bf16" | "mxfp4": bf16 tensors whose layer matrices are kept in 4 bits)."""
     return ModelConfig(shape.n_layers, shape.hidden, shape.n_q_heads, shape.n_kv_heads, shape.head_dim, shape.ffn,
-                       shape.vocab, max_seq, shape.rms_eps, shape.rope_theta, F32 if shape.dtype == "fp32" else BF16)
+                       shape.vocab, max_seq, shape.rms_eps, shape.rope_theta, _MODEL_DTYPES[shape.dtype])
 
 
 def check_config(cfg: ModelConfig) -> int:

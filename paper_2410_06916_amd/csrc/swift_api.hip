@@ -13,6 +13,7 @@
 #include <vector>
 
 #include "swift_kernels.h"
+#include "swift_mx4.h"
 
 using namespace swift;
 
@@ -25,6 +26,7 @@ static int fail(int code, const std::string &msg) {
     g_err = msg;
     return code;
 }
+int swift::api_fail(int code, const std::string &msg) { return fail(code, msg); }
 
 #define HIP_TRY(expr)                                                                                   \
     do {                                                                                                \
@@ -40,13 +42,15 @@ extern "C" const char *swift_last_error(void) { return g_err.c_str(); }
 // ------------------------------------------------------------------------------------------
 static inline uint64_t align_up(uint64_t v, uint64_t a = 256) { return (v + a - 1) / a * a; }
 static inline int elem_bytes(int dtype) { return dtype == SWIFT_F32 ? 4 : 2; }
+// What the key/value cache, the embedding and the LM head are stored in.
+static inline int store_dtype(const swift_model_config &c) { return c.dtype == SWIFT_F32 ? SWIFT_F32 : SWIFT_BF16; }
 
 extern "C" int swift_check_config(const swift_model_config *c) {
     if (!c) return fail(SWIFT_EINVAL, "null config");
     if (c->n_layers <= 0 || c->hidden <= 0 || c->n_q_heads <= 0 || c->n_kv_heads <= 0 || c->head_dim <= 0 ||
         c->ffn <= 0 || c->vocab <= 0 || c->max_seq <= 0)
         return fail(SWIFT_EINVAL, "sizes must be positive");
-    if (c->dtype != SWIFT_F32 && c->dtype != SWIFT_BF16) return fail(SWIFT_EINVAL, "unknown dtype");
+    if (c->dtype != SWIFT_F32 && c->dtype != SWIFT_BF16 && c->dtype != SWIFT_MXFP4) return fail(SWIFT_EINVAL, "unknown dtype");
     const int d = c->head_dim;
     if (!(d == 16 || d == 32 || d == 64 || d == 128)) return fail(SWIFT_EINVAL, "head_dim must be 16, 32, 64 or 128");
     if (c->n_q_heads % c->n_kv_heads) return fail(SWIFT_EINVAL, "n_q_heads must be a multiple of n_kv_heads");
@@ -64,7 +68,7 @@ extern "C" int swift_check_config(const swift_model_config *c) {
 namespace {
 
 struct LayerOff {
-    uint64_t attn_norm, wqkv, wo, mlp_norm, wgu, wd;
+    uint64_t attn_norm, wqkv, wo, mlp_norm, wgu, wd;  // (MXFP4: a matrix's scales follow its codes)
 };
 
 struct Layout {
@@ -88,6 +92,7 @@ struct Layout {
     // bf16 matrices whose activation row fits the MFMA kernel's LDS budget are stored tiled
     bool tiled_h, tiled_q, tiled_f;  // for K = hidden, K = n_q*d, K = ffn
     bool tiled;                      // all three: the whole model runs on the tiled MFMA kernels
+    bool mx4;                        // the layers' projections are MXFP4 matrices (swift_mx4.h), tiled as the others otherwise
 };
 
 inline uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
@@ -107,8 +112,13 @@ Layout make_layout(const swift_model_config &c) {
         off = align_up(off + bytes);
         return o;
     };
-    const bool bf = c.dtype == SWIFT_BF16;
-    // bf16 models run on the tiled MFMA kernels (a depth too large for the LDS-resident kernel goes
+    const bool bf = c.dtype != SWIFT_F32;
+    L.mx4 = c.dtype == SWIFT_MXFP4;
+    // A projection of n_rg row groups, as [rows][K] in row-major storage.
+    auto matrix = [&](uint64_t n_rg, uint64_t rows, uint64_t K) {
+        return take(L.mx4 ? mx4_code_bytes(n_rg, (int)K) + mx4_scale_bytes(n_rg, (int)K) : bf ? tiled_bytes(n_rg, K) : rows * K * eb);
+    };
+    // bf16 and MXFP4 models run on the tiled MFMA kernels (a depth too large for the LDS-resident kernel goes
     // through the block kernels, whatever the row count)
     L.tiled = bf;
     L.tiled_h = L.tiled_q = L.tiled_f = L.tiled;
@@ -118,15 +128,15 @@ Layout make_layout(const swift_model_config &c) {
     L.layers.resize(c.n_layers);
     for (auto &y : L.layers) {
         y.attn_norm = take(H * 4);
-        y.wqkv = take(L.tiled_h ? tiled_bytes((Q + 2 * KV) / 16, H) : (Q + 2 * KV) * H * eb);
-        y.wo = take(L.tiled_q ? tiled_bytes(ceil_div(H, 16), Q) : H * Q * eb);
+        y.wqkv = matrix((Q + 2 * KV) / 16, Q + 2 * KV, H);
+        y.wo = matrix(ceil_div(H, 16), H, Q);
         y.mlp_norm = take(H * 4);
-        y.wgu = take(L.tiled_h ? tiled_bytes(ceil_div(F, 8), H) : 2 * F * H * eb);
-        y.wd = take(L.tiled_f ? tiled_bytes(ceil_div(H, 16), F) : H * F * eb);
+        y.wgu = matrix(ceil_div(F, 8), 2 * F, H);
+        y.wd = matrix(ceil_div(H, 16), H, F);
     }
     L.cos = take((uint64_t)c.max_seq * (c.head_dim / 2) * 4);
     L.sin = take((uint64_t)c.max_seq * (c.head_dim / 2) * 4);
-    L.mfma_attn = attn_mfma_applies(c.dtype, c.head_dim);
+    L.mfma_attn = attn_mfma_applies(store_dtype(c), c.head_dim);
     L.nb32 = L.mfma_attn ? (c.max_seq + 31) / 32 : 0;
     L.kv_k_bytes = align_up(KV * c.max_seq * eb);
     L.kv_v_bytes = align_up(L.mfma_attn ? KV * (uint64_t)L.nb32 * 32 * eb : KV * c.max_seq * eb);
@@ -190,13 +200,17 @@ namespace {
 struct SubBytes {
     uint64_t attn_w, mlp_w, head_w, kv_slot;  // kv_slot: one slot of one layer (K and V)
 };
+// A projection [rows][K] (MXFP4: 16 bytes of codes and a scale for every 32 weights of a row).
+uint64_t weight_bytes(int dtype, uint64_t rows, uint64_t K) {
+    return dtype == SWIFT_MXFP4 ? rows * ceil_div(K, kMx4Block) * (kMx4Block / 2 + 1) : rows * K * elem_bytes(dtype);
+}
 SubBytes sub_bytes(const swift_model_config &c) {
     const uint64_t eb = elem_bytes(c.dtype);
     const uint64_t H = c.hidden, Q = (uint64_t)c.n_q_heads * c.head_dim, KV = (uint64_t)c.n_kv_heads * c.head_dim,
                    F = c.ffn, V = c.vocab;
     SubBytes b;
-    b.attn_w = (Q + 2 * KV) * H * eb + H * Q * eb + H * 4;
-    b.mlp_w = 3 * F * H * eb + H * 4;
+    b.attn_w = weight_bytes(c.dtype, Q + 2 * KV, H) + weight_bytes(c.dtype, H, Q) + H * 4;
+    b.mlp_w = weight_bytes(c.dtype, 2 * F, H) + weight_bytes(c.dtype, H, F) + H * 4;
     b.head_w = V * H * eb + H * 4;
     b.kv_slot = 2 * KV * eb;
     return b;
@@ -439,7 +453,7 @@ int forward_block_rows(swift_ctx *x, const int32_t *tokens, int R, int pos0, con
                     a.tt = *tree;
                 }
                 HIP_TRY(timed(x, SWIFT_KC_ATTN, (uint64_t)2 * KV * eb * (pos0 + row0 + a.rows),
-                              [&] { return launch_attn_decode(c.dtype, a, x->n_cu, s); }));
+                              [&] { return launch_attn_decode(store_dtype(c), a, x->n_cu, s); }));
             }
             if ((rc = linear(SWIFT_KC_OPROJ, EPI_RESID, y.wo, H, Q, ar, nullptr, xr, H, l))) return rc;
         }
@@ -463,7 +477,7 @@ int block_attention(swift_ctx *x, const AttnArgs &at, int RLC) {
     const Layout &L = x->L;
     hipStream_t s = x->stream;
     const int R = at.rows, Q = c.n_q_heads * c.head_dim, KV = c.n_kv_heads * c.head_dim, ctx0 = at.n_ctx - 1;
-    if (attn_block_applies(c.dtype, at)) {
+    if (attn_block_applies(store_dtype(c), at)) {
         AttnArgs a = at;
         a.out_rows = RLC;
         HIP_TRY(timed(x, SWIFT_KC_ATTN, (uint64_t)2 * KV * 2 * (ctx0 + R), [&] { return launch_attn_block(a, x->n_cu, s); }));
@@ -483,7 +497,7 @@ int block_attention(swift_ctx *x, const AttnArgs &at, int RLC) {
             a.out_s += 8 * block_terms(RLC) * row0;  // first of this part's term columns
             a.out_rows = RLC;
             HIP_TRY(timed(x, SWIFT_KC_ATTN, (uint64_t)2 * KV * 2 * (ctx0 + row0 + a.rows),
-                          [&] { return launch_attn_decode(c.dtype, a, x->n_cu, s); }));
+                          [&] { return launch_attn_decode(store_dtype(c), a, x->n_cu, s); }));
         }
     }
     return SWIFT_OK;
@@ -611,14 +625,25 @@ int forward_block_tiled(swift_ctx *x, const int32_t *tokens, int R, int pos0, co
 
     // ---- one launch per stage, issued as soon as its arguments stand: the device starts on the first one while the host
     // prepares the others
-    auto run_mv = [&](int kc, int epi, const MvArgs &m) -> int {
-        if (n_sub > 0 && epi != EPI_LOGITS && !tail) {
+    // (rg0: an MXFP4 matrix's first row group of the launch)
+    auto run_mv = [&](int kc, int epi, const MvArgs &m, int rg0 = 0) -> int {
+        const bool macro = n_sub > 0 && epi != EPI_LOGITS && !tail;
+        if (macro) {
             // (sub-block strides: which buffers a launch reads and writes follows from its epilogue)
             ma.in_s = kc == SWIFT_KC_OPROJ ? L.sub_as : kc == SWIFT_KC_DOWN ? L.sub_hs : L.sub_xs;
             ma.pss = L.sub_pss;
             ma.out_f32 = epi == EPI_QKV ? L.sub_q : L.sub_x;
             ma.out_s = epi == EPI_SWIGLU ? L.sub_hs : L.sub_xs;
             ma.pss_out = L.sub_pss;
+        }
+        if (L.mx4 && epi != EPI_LOGITS) {
+            const int all = kc == SWIFT_KC_QKV ? (Q + 2 * KV) / 16 : m.n_rg;
+            const auto *codes = (const uint8_t *)(const void *)m.Wt;
+            const Mx4Matrix w{codes, codes + mx4_code_bytes(all, m.K), mx4_tiles(m.K), all};
+            HIP_TRY(timed(x, kc, weight_bytes(c.dtype, m.O - 16 * rg0, m.K), [&] {
+                return macro ? launch_mx4_macro(epi, m, ma, w, rg0, s) : launch_mx4_mv(epi, m, w, rg0, s);
+            }));
+        } else if (macro) {
             HIP_TRY(timed(x, kc, (uint64_t)m.O * m.K * 2, [&] { return launch_gemm(epi, m, ma, x->n_cu, x->gemm_rgw, s); }));
         } else {
             HIP_TRY(timed(x, kc, (uint64_t)m.O * m.K * 2,
@@ -662,7 +687,7 @@ int forward_block_tiled(swift_ctx *x, const int32_t *tokens, int R, int pos0, co
         if (i == tail_stage) {
             // keys and values of all rows
             MvArgs m = base_args(y.wqkv, Q + 2 * KV, H, (Q + 2 * KV) / 16);
-            last_layer_rows(c, x->n_cu, m, ma);
+            if (!L.mx4) last_layer_rows(c, x->n_cu, m, ma);
             m.out_f32 = qf;
             m.ld_out = Q;
             m.in_s = xs;
@@ -671,7 +696,7 @@ int forward_block_tiled(swift_ctx *x, const int32_t *tokens, int R, int pos0, co
             m.kcache = kv_base(x, l, 0);
             m.vcache = kv_base(x, l, 1);
             m.nb32 = L.nb32;
-            if (int rc = run_mv(SWIFT_KC_QKV, EPI_QKV, m)) return rc;
+            if (int rc = run_mv(SWIFT_KC_QKV, EPI_QKV, m, L.mx4 ? Q / 16 : 0)) return rc;
             if (!want_logits) return SWIFT_OK;
             ma.matrix_rg = ma.first_rg = 0;
             // from here on: the last sub-block's rows and buffers
@@ -860,6 +885,7 @@ struct Slot {
     bool tiled;         // destination is in the tiled MFMA layout
     int tile_mode, part;
     int n_rg;           // row groups this tensor fills
+    uint64_t scales;    // MXFP4 destination: where its scales go (0: a bf16 one)
 };
 
 bool find_slot(swift_ctx *x, const char *name, Slot *out) {
@@ -868,18 +894,23 @@ bool find_slot(swift_ctx *x, const char *name, Slot *out) {
     const uint64_t eb = elem_bytes(c.dtype);
     const int H = c.hidden, d = c.head_dim, Q = c.n_q_heads * d, KV = c.n_kv_heads * d, F = c.ffn, V = c.vocab;
     auto mat = [&](int idx, uint64_t off, int r, int k, uint64_t pitch = 0) {
-        *out = Slot{idx, off, (int64_t)r * k, false, r, k, pitch, false, 0, 0, 0};
+        *out = Slot{idx, off, (int64_t)r * k, false, r, k, pitch, false, 0, 0, 0, 0};
         return true;
     };
     auto tiled = [&](int idx, uint64_t off, int r, int k, int mode, int part, int n_rg) {
-        *out = Slot{idx, off, (int64_t)r * k, false, r, k, 0, true, mode, part, n_rg};
+        *out = Slot{idx, off, (int64_t)r * k, false, r, k, 0, true, mode, part, n_rg, 0};
+        return true;
+    };
+    // Row groups rg0 .. of a layer's matrix of `all` row groups.
+    auto layer = [&](int idx, uint64_t off, int r, int k, int mode, int part, int n_rg, int rg0, int all) {
+        tiled(idx, off + (L.mx4 ? mx4_code_bytes(rg0, k) : tiled_bytes(rg0, k)), r, k, mode, part, n_rg);
+        if (L.mx4) out->scales = off + mx4_code_bytes(all, k) + mx4_scale_bytes(rg0, k);
         return true;
     };
     auto gain = [&](int idx, uint64_t off) {
-        *out = Slot{idx, off, H, true, 1, H, 0, false, 0, 0, 0};
+        *out = Slot{idx, off, H, true, 1, H, 0, false, 0, 0, 0, 0};
         return true;
     };
-    const uint64_t TH = (uint64_t)((H + 31) / 32) * 1024;  // bytes of one row group with K = hidden
     if (!strcmp(name, "embed")) return mat(0, L.embed, V, H);
     if (!strcmp(name, "lm_head"))
         return L.tiled_h ? tiled(1, L.lm_head, V, H, TILE_PLAIN, 0, (V + 15) / 16) : mat(1, L.lm_head, V, H);
@@ -894,12 +925,12 @@ bool find_slot(swift_ctx *x, const char *name, Slot *out) {
     if (!strcmp(f, "attn_norm")) return gain(b + 0, y.attn_norm);
     if (L.tiled_h) {
         // fused q|k|v, rotary pairs in one row group; d/16 row groups per head
-        if (!strcmp(f, "wq")) return tiled(b + 1, y.wqkv, Q, H, TILE_PAIR, 0, Q / 16);
-        if (!strcmp(f, "wk")) return tiled(b + 2, y.wqkv + (uint64_t)(Q / 16) * TH, KV, H, TILE_PAIR, 0, KV / 16);
-        if (!strcmp(f, "wv"))
-            return tiled(b + 3, y.wqkv + (uint64_t)((Q + KV) / 16) * TH, KV, H, TILE_PAIR, 0, KV / 16);
-        if (!strcmp(f, "wg")) return tiled(b + 6, y.wgu, F, H, TILE_GATEUP, 0, (F + 7) / 8);
-        if (!strcmp(f, "wu")) return tiled(b + 7, y.wgu, F, H, TILE_GATEUP, 1, (F + 7) / 8);
+        const int nq = Q / 16, nkv = KV / 16, gu = (F + 7) / 8;
+        if (!strcmp(f, "wq")) return layer(b + 1, y.wqkv, Q, H, TILE_PAIR, 0, nq, 0, nq + 2 * nkv);
+        if (!strcmp(f, "wk")) return layer(b + 2, y.wqkv, KV, H, TILE_PAIR, 0, nkv, nq, nq + 2 * nkv);
+        if (!strcmp(f, "wv")) return layer(b + 3, y.wqkv, KV, H, TILE_PAIR, 0, nkv, nq + nkv, nq + 2 * nkv);
+        if (!strcmp(f, "wg")) return layer(b + 6, y.wgu, F, H, TILE_GATEUP, 0, gu, 0, gu);
+        if (!strcmp(f, "wu")) return layer(b + 7, y.wgu, F, H, TILE_GATEUP, 1, gu, 0, gu);
     } else {
         if (!strcmp(f, "wq")) return mat(b + 1, y.wqkv, Q, H);
         if (!strcmp(f, "wk")) return mat(b + 2, y.wqkv + (uint64_t)Q * H * eb, KV, H);
@@ -908,9 +939,9 @@ bool find_slot(swift_ctx *x, const char *name, Slot *out) {
         if (!strcmp(f, "wg")) return mat(b + 6, y.wgu, F, H, 2 * (uint64_t)H * eb);
         if (!strcmp(f, "wu")) return mat(b + 7, y.wgu + (uint64_t)H * eb, F, H, 2 * (uint64_t)H * eb);
     }
-    if (!strcmp(f, "wo")) return L.tiled_q ? tiled(b + 4, y.wo, H, Q, TILE_PLAIN, 0, (H + 15) / 16) : mat(b + 4, y.wo, H, Q);
+    if (!strcmp(f, "wo")) return L.tiled_q ? layer(b + 4, y.wo, H, Q, TILE_PLAIN, 0, (H + 15) / 16, 0, (H + 15) / 16) : mat(b + 4, y.wo, H, Q);
     if (!strcmp(f, "mlp_norm")) return gain(b + 5, y.mlp_norm);
-    if (!strcmp(f, "wd")) return L.tiled_f ? tiled(b + 8, y.wd, H, F, TILE_PLAIN, 0, (H + 15) / 16) : mat(b + 8, y.wd, H, F);
+    if (!strcmp(f, "wd")) return L.tiled_f ? layer(b + 8, y.wd, H, F, TILE_PLAIN, 0, (H + 15) / 16, 0, (H + 15) / 16) : mat(b + 8, y.wd, H, F);
     return false;
 }
 
@@ -1013,7 +1044,7 @@ extern "C" int swift_load_tensor(swift_ctx *x, const char *name, const void *dat
     Slot sl;
     if (!find_slot(x, name, &sl)) return fail(SWIFT_EINVAL, std::string("unknown tensor name: ") + name);
     if (n_elems != sl.n) return fail(SWIFT_EINVAL, std::string("wrong element count for ") + name);
-    const int want = sl.is_gain ? SWIFT_F32 : x->c.dtype;
+    const int want = sl.is_gain ? SWIFT_F32 : store_dtype(x->c);
     if (dtype != want) return fail(SWIFT_EINVAL, std::string("wrong dtype for ") + name);
     const uint64_t eb = elem_bytes(want);
     if (sl.tiled) {
@@ -1028,17 +1059,23 @@ extern "C" int swift_load_tensor(swift_ctx *x, const char *name, const void *dat
             HIP_TRY(hipMemcpyAsync(x->base + x->L.stage, data, (uint64_t)sl.n * eb, hipMemcpyHostToDevice, x->stream));
             src = x->base + x->L.stage;
         }
-        TileArgs t{};
-        t.src = src;
-        t.src_rows = sl.rows;
-        t.K = sl.cols;
-        t.dst = x->base + sl.off;
-        t.T = (sl.cols + 31) / 32;
-        t.n_rg = sl.n_rg;
-        t.mode = sl.tile_mode;
-        t.head_dim = x->c.head_dim;
-        t.part = sl.part;
-        HIP_TRY(launch_tile_weights(t, x->stream));
+        if (sl.scales != 0) {
+            const Mx4QuantArgs q{src,       SWIFT_BF16,   sl.cols,          sl.rows, sl.cols, (uint8_t *)x->base + sl.off, (uint8_t *)x->base + sl.scales,
+                                 sl.n_rg,   sl.tile_mode, x->c.head_dim,    sl.part};
+            HIP_TRY(launch_mx4_quantize(q, x->stream));
+        } else {
+            TileArgs t{};
+            t.src = src;
+            t.src_rows = sl.rows;
+            t.K = sl.cols;
+            t.dst = x->base + sl.off;
+            t.T = (sl.cols + 31) / 32;
+            t.n_rg = sl.n_rg;
+            t.mode = sl.tile_mode;
+            t.head_dim = x->c.head_dim;
+            t.part = sl.part;
+            HIP_TRY(launch_tile_weights(t, x->stream));
+        }
     } else if (sl.dst_pitch == 0) {
         HIP_TRY(hipMemcpyAsync(x->base + sl.off, data, (uint64_t)sl.n * eb, hipMemcpyDefault, x->stream));
     } else {
@@ -1257,7 +1294,7 @@ extern "C" int swift_verify_static(swift_ctx *x, const int32_t *tokens, int k, i
         a.n_kv_heads = c.n_kv_heads;
         a.max_split = x->L.n_split_max;
         a.nb32 = x->L.nb32;
-        attn_floats = x->L.mfma_attn ? attn_mfma_partial_floats(a, x->n_cu) : attn_partial_floats(c.dtype, a, x->n_cu);
+        attn_floats = x->L.mfma_attn ? attn_mfma_partial_floats(a, x->n_cu) : attn_partial_floats(store_dtype(c), a, x->n_cu);
     }
     // part_o then holds attn_floats floats and part_ml two per head_dim of them
     const size_t ml_bytes = align_up(attn_floats / d * 2 * 4);
@@ -1266,11 +1303,12 @@ extern "C" int swift_verify_static(swift_ctx *x, const int32_t *tokens, int k, i
                                          " rows of this model need " + std::to_string(ml_bytes + attn_floats * 4) +
                                          " bytes, the static scratch holds " + std::to_string(kStaticAttnBytes) +
                                          "; use swift_verify");
-    if (x->L.tiled) {
+    if (x->L.tiled) {  // (MXFP4 projections need none: only the LM head does)
         const struct { int O, K, n_rg; } mats[5] = {{Q + 2 * KV, H, (Q + 2 * KV) / 16}, {H, Q, (H + 15) / 16},
                                                     {2 * F, H, (F + 7) / 8},             {H, F, (H + 15) / 16},
                                                     {V, H, (V + 15) / 16}};
         for (const auto &mt : mats) {
+            if (x->L.mx4 && &mt != &mats[4]) continue;
             MvArgs m{};
             m.O = mt.O;
             m.K = mt.K;
@@ -1438,7 +1476,7 @@ extern "C" int swift_accept_tree(swift_ctx *x, int32_t *emitted, int *n_emitted)
         mv.n_kv_heads = c.n_kv_heads;
         mv.max_seq = c.max_seq;
         mv.head_dim = c.head_dim;
-        HIP_TRY(launch_kv_move(c.dtype, mv, x->stream));
+        HIP_TRY(launch_kv_move(store_dtype(c), mv, x->stream));
     }
     emitted[acc] = cur;
     *n_emitted = acc + 1;
@@ -1637,7 +1675,7 @@ extern "C" int swift_debug_poison_kv(swift_ctx *x) {
             }
             for (int g = 0; g < c.n_kv_heads; ++g) {
                 char *p = kv_base(x, l, w) + ((uint64_t)g * c.max_seq + x->n) * c.head_dim * eb;
-                HIP_TRY(launch_fill_nan(c.dtype, p, tail, x->stream));
+                HIP_TRY(launch_fill_nan(store_dtype(c), p, tail, x->stream));
             }
         }
     HIP_TRY(hipStreamSynchronize(x->stream));
@@ -1665,7 +1703,7 @@ extern "C" int swift_debug_read_kv(swift_ctx *x, int layer, int pos, float *k_ou
         } else {
             for (int g = 0; g < c.n_kv_heads; ++g) {
                 const char *src = kv_base(x, layer, w) + ((uint64_t)g * c.max_seq + pos) * c.head_dim * eb;
-                HIP_TRY(launch_to_f32(c.dtype, src, tmp + (size_t)g * c.head_dim, c.head_dim, x->stream));
+                HIP_TRY(launch_to_f32(store_dtype(c), src, tmp + (size_t)g * c.head_dim, c.head_dim, x->stream));
             }
         }
         HIP_TRY(hipMemcpyAsync(w == 0 ? k_out : v_out, tmp, (size_t)c.n_kv_heads * c.head_dim * 4, hipMemcpyDeviceToHost,
@@ -1692,12 +1730,12 @@ extern "C" int swift_debug_attn_path(swift_ctx *x, int rows, int tree, char *out
     a.nb32 = x->L.nb32;
     if (tree)  // (a chain of `rows` levels: the deepest tree of that many rows)
         for (int r = 0; r < rows; ++r) a.tt.depth[r] = a.tt.spine[r] = (uint8_t)r;
-    if (x->L.tiled && attn_block_applies(c.dtype, a))
+    if (x->L.tiled && attn_block_applies(store_dtype(c), a))
         snprintf(out, (size_t)capacity, "block<bf16, d %d>", c.head_dim);
     else if (x->L.mfma_attn)
         attn_mfma_path_name(a, x->n_cu, out, capacity);
     else
-        attn_path_name(c.dtype, a, x->n_cu, out, capacity);
+        attn_path_name(store_dtype(c), a, x->n_cu, out, capacity);
     return SWIFT_OK;
 }
 

@@ -6,9 +6,14 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <string>
+
 #include "../../include/swift.h"
 
 namespace swift {
+
+// Sets the text of swift_last_error and returns code (for the C-ABI layers).
+int api_fail(int code, const std::string &msg);
 
 constexpr int kMaxRows = 32;       // rows of one verify block or token tree (SWIFT_MAX_BLOCK)
 constexpr int kMaxBlockRows = 64;  // rows of one prefill block

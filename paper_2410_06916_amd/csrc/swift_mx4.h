@@ -1,0 +1,96 @@
+// MXFP4 matrices: launch interface between the C-ABI layers and the kernels of swift_mx4_pack.hip and swift_mx4.hip.
+//
+// The format (OCP Microscaling Formats v1.0): 32 consecutive weights of a row share the scale 2^(e - 127), e one byte; an element is
+// four bits, a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6.  e = 255: the block is NaN.  A row's last block holds what is left of it.
+//
+// A packed matrix [O][K] is a plane of codes and a plane of scales behind it, both cut into pieces of 16 rows (a row group, rows as
+// TileMode says) x 128 k (a super-tile), piece (rg, s) at number rg S + s, S = ceil(K / 128):
+//   codes   1 KB: lane l = 16 kg + j of a wavefront owns the 16 bytes of one block, tile row j, k = 128 s + 32 kg .. + 31, the
+//           earlier weight of a byte in its low half;
+//   scales  64 bytes: lane l's is that block's.
+// So one 128-bit load per lane is a whole block with one scale, and word t of it (k = 32 kg + 8 t ..) is, converted, the A operand of the
+// t-th of four v_mfma_f32_16x16x32_bf16, whose B operand lane (kg, column) then holds k = 128 s + 32 kg + 8 t .. + 7: the reduction index
+// is permuted within 128 on both sides alike, which costs nothing.  Rows and k past the matrix are zero codes.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "swift_kernels.h"
+
+namespace swift {
+
+constexpr int kMx4Block = 32, kMx4Tile = 128;
+__host__ __device__ inline int mx4_tiles(int K) { return (K + kMx4Tile - 1) / kMx4Tile; }
+inline uint64_t mx4_code_bytes(uint64_t n_rg, int K) { return n_rg * mx4_tiles(K) * 1024; }
+inline uint64_t mx4_scale_bytes(uint64_t n_rg, int K) { return n_rg * mx4_tiles(K) * 64; }
+
+struct Mx4Matrix {
+    const uint8_t *codes, *scales;
+    int S;      // super-tiles of a row group
+    int n_rg;   // row groups
+};
+
+// ---- packing (swift_mx4_pack.hip)
+struct Mx4QuantArgs {
+    const void *src;  // [src_rows][K], rows ld elements apart
+    int dtype;        // F32 or BF16
+    int64_t ld;
+    int src_rows, K;
+    uint8_t *codes, *scales;  // first row group written
+    int n_rg, mode, head_dim, part;  // as in TileArgs
+};
+hipError_t launch_mx4_quantize(const Mx4QuantArgs &a, hipStream_t s);
+
+struct Mx4DequantArgs {
+    Mx4Matrix w;
+    void *dst;  // [rows][K] (TILE_GATEUP: the gate rows, then the up rows), rows ld elements apart
+    int dtype;
+    int64_t ld;
+    int rows, K, mode;  // rows: of the matrix (TILE_GATEUP: of each half); TILE_PLAIN or TILE_GATEUP
+};
+hipError_t launch_mx4_dequantize(const Mx4DequantArgs &a, hipStream_t s);
+
+// Activations [n][K] to the B operand's layout [16 S chunks][NC columns][8 k] bf16, zeros past K: a bf16 row is one column, an fp32 row
+// three (value = hi + mid + lo; column 3 r + term).
+inline int mx4_terms(int dtype) { return dtype == F32 ? 3 : 1; }
+struct Mx4ActArgs {
+    const void *x;
+    int dtype;
+    int64_t ld;
+    int n, K, S;
+    uint16_t *out;
+};
+hipError_t launch_mx4_activations(const Mx4ActArgs &a, hipStream_t s);
+
+// ---- products (swift_mx4.hip)
+// What follows the dot products of a call that is not part of a model's pass, beside Epilogue's.
+enum Mx4Epilogue : int {
+    EPI_LINEAR = 8,  // y = W x (+ residual)
+    EPI_GATED = 9,   // h = silu(gate) * up
+};
+struct Mx4Out {
+    void *y;
+    int dtype;
+    int64_t ld;
+    const void *residual;  // nullptr, or of y's type
+    int64_t ld_res;
+};
+// Rows of a launch: as many columns as eight column blocks hold.
+constexpr int kMx4MaxColumns = 128;
+
+// A model's projection (epilogue: EPI_QKV, EPI_RESID or EPI_SWIGLU) of a block of a.R rows, as launch_mv, over the row groups [rg0, a.n_rg) of w.
+hipError_t launch_mx4_mv(int epilogue, const MvArgs &a, const Mx4Matrix &w, int rg0, hipStream_t s);
+// The same for a prompt macro block, as launch_gemm.
+hipError_t launch_mx4_macro(int epilogue, const MvArgs &a, const MacroArgs &ma, const Mx4Matrix &w, int rg0, hipStream_t s);
+// A call's product: n rows (columns as launch_mx4_activations lays them out, at most kMx4MaxColumns) against w, O results a row
+// (EPI_GATED: of the gate and the up half each).
+struct Mx4CallArgs {
+    Mx4Matrix w;
+    const uint16_t *x;
+    int n, terms, O;
+    Mx4Out out;
+};
+hipError_t launch_mx4_call(int epilogue, const Mx4CallArgs &a, hipStream_t s);
+
+}  // namespace swift

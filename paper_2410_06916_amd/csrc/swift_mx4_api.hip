@@ -1,0 +1,137 @@
+// C-ABI layer of the MXFP4 operators (declared in include/swift.h): checks of arguments, sizes, and the launches a call is made of.
+#include <algorithm>
+
+#include "swift_mx4.h"
+
+using namespace swift;
+
+namespace {
+
+constexpr int kMaxSide = 1 << 22;  // rows and depth of a packed matrix
+
+int device_status(hipError_t e, const char *what) {
+    return e == hipSuccess ? SWIFT_OK : api_fail(SWIFT_EDEVICE, std::string(what) + ": " + hipGetErrorString(e));
+}
+
+int check_matrix(int rows, int depth) {
+    if (rows < 1 || depth < 1 || rows > kMaxSide || depth > kMaxSide)
+        return api_fail(SWIFT_EINVAL, "a packed matrix has 1 to 2^22 rows and a depth of 1 to 2^22");
+    return SWIFT_OK;
+}
+bool known_dtype(int t) { return t == SWIFT_F32 || t == SWIFT_BF16; }
+bool aligned(const void *p, int dtype) { return ((uintptr_t)p & (dtype == SWIFT_F32 ? 3 : 1)) == 0; }
+
+int row_groups(int rows, bool gated) { return gated ? (rows + 7) / 8 : (rows + 15) / 16; }
+Mx4Matrix matrix_at(const void *packed, int rows, int depth, bool gated) {
+    const int n_rg = row_groups(rows, gated);
+    const auto *codes = (const uint8_t *)packed;
+    return Mx4Matrix{codes, codes + mx4_code_bytes(n_rg, depth), mx4_tiles(depth), n_rg};
+}
+
+// Rows of x that one launch takes.
+int launch_rows(int x_dtype) { return kMx4MaxColumns / mx4_terms(x_dtype); }
+uint64_t workspace(int depth, int n, int x_dtype) {
+    return (uint64_t)mx4_tiles(depth) * kMx4Tile * mx4_terms(x_dtype) * std::min(n, launch_rows(x_dtype)) * 2;
+}
+
+struct Call {
+    void *y;
+    int y_dtype;
+    int64_t ld_y;
+    const void *x;
+    int x_dtype;
+    int64_t ld_x;
+    const void *packed;
+    int rows, depth, n;
+    const void *residual;
+    int64_t ld_res;
+    void *ws;
+    uint64_t ws_bytes;
+};
+
+int product(int epi, const Call &c, void *stream) {
+    if (int rc = check_matrix(c.rows, c.depth)) return rc;
+    if (c.n < 0) return api_fail(SWIFT_EINVAL, "a negative number of rows");
+    if (!known_dtype(c.x_dtype) || !known_dtype(c.y_dtype)) return api_fail(SWIFT_EINVAL, "unknown dtype");
+    if (c.n == 0) return SWIFT_OK;
+    if (!c.y || !c.x || !c.packed) return api_fail(SWIFT_EINVAL, "null argument");
+    if (c.ld_x < c.depth || c.ld_y < c.rows || (c.residual && c.ld_res < c.rows)) return api_fail(SWIFT_EINVAL, "rows overlap: a leading dimension is too small");
+    if (!aligned(c.x, c.x_dtype) || !aligned(c.y, c.y_dtype) || (c.residual && !aligned(c.residual, c.y_dtype)) || ((uintptr_t)c.packed & 255))
+        return api_fail(SWIFT_EINVAL, "a pointer is not aligned to its elements (a packed matrix: to 256 bytes)");
+    const uint64_t need = workspace(c.depth, c.n, c.x_dtype);
+    if (!c.ws || ((uintptr_t)c.ws & 255) || c.ws_bytes < need)
+        return api_fail(SWIFT_ECAPACITY, "the workspace is missing, not aligned to 256 bytes, or smaller than swift_mx4_workspace says");
+    const auto s = (hipStream_t)stream;
+    const int per = launch_rows(c.x_dtype), xb = c.x_dtype == SWIFT_F32 ? 4 : 2, yb = c.y_dtype == SWIFT_F32 ? 4 : 2;
+    Mx4CallArgs a{};
+    a.w = matrix_at(c.packed, c.rows, c.depth, epi == EPI_GATED);
+    a.x = (const uint16_t *)c.ws;
+    a.terms = mx4_terms(c.x_dtype);
+    a.O = c.rows;
+    for (int r0 = 0; r0 < c.n; r0 += per) {
+        a.n = std::min(per, c.n - r0);
+        Mx4ActArgs act{(const char *)c.x + r0 * c.ld_x * xb, c.x_dtype, c.ld_x, a.n, c.depth, a.w.S, (uint16_t *)c.ws};
+        if (int rc = device_status(launch_mx4_activations(act, s), "activations of an MXFP4 product")) return rc;
+        a.out = Mx4Out{(char *)c.y + r0 * c.ld_y * yb, c.y_dtype, c.ld_y, c.residual ? (const char *)c.residual + r0 * c.ld_res * yb : nullptr, c.ld_res};
+        if (int rc = device_status(launch_mx4_call(epi, a, s), "MXFP4 product")) return rc;
+    }
+    return SWIFT_OK;
+}
+
+}  // namespace
+
+extern "C" int swift_mx4_bytes(int rows, int depth, int gated, uint64_t *bytes) {
+    if (!bytes) return api_fail(SWIFT_EINVAL, "null output");
+    if (int rc = check_matrix(rows, depth)) return rc;
+    const int n_rg = row_groups(rows, gated != 0);
+    *bytes = mx4_code_bytes(n_rg, depth) + mx4_scale_bytes(n_rg, depth);
+    return SWIFT_OK;
+}
+
+extern "C" int swift_mx4_workspace(int rows, int depth, int gated, int n, int x_dtype, uint64_t *bytes) {
+    (void)gated;
+    if (!bytes) return api_fail(SWIFT_EINVAL, "null output");
+    if (int rc = check_matrix(rows, depth)) return rc;
+    if (n < 0 || !known_dtype(x_dtype)) return api_fail(SWIFT_EINVAL, "bad argument");
+    *bytes = workspace(depth, n, x_dtype);
+    return SWIFT_OK;
+}
+
+extern "C" int swift_mx4_quantize(void *packed, const void *w, int64_t ld_w, const void *up, int64_t ld_up, int dtype, int rows, int depth,
+                                  void *stream) {
+    if (!packed || !w) return api_fail(SWIFT_EINVAL, "null argument");
+    if (int rc = check_matrix(rows, depth)) return rc;
+    if (!known_dtype(dtype)) return api_fail(SWIFT_EINVAL, "unknown dtype");
+    if (ld_w < depth || (up && ld_up < depth)) return api_fail(SWIFT_EINVAL, "rows overlap: a leading dimension is too small");
+    if (((uintptr_t)packed & 255) || !aligned(w, dtype) || (up && !aligned(up, dtype)))
+        return api_fail(SWIFT_EINVAL, "a pointer is not aligned to its elements (a packed matrix: to 256 bytes)");
+    const Mx4Matrix m = matrix_at(packed, rows, depth, up != nullptr);
+    Mx4QuantArgs a{w, dtype, ld_w, rows, depth, (uint8_t *)m.codes, (uint8_t *)m.scales, m.n_rg, up ? TILE_GATEUP : TILE_PLAIN, 0, 0};
+    int rc = device_status(launch_mx4_quantize(a, (hipStream_t)stream), "swift_mx4_quantize");
+    if (rc || !up) return rc;
+    a.src = up;
+    a.ld = ld_up;
+    a.part = 1;
+    return device_status(launch_mx4_quantize(a, (hipStream_t)stream), "swift_mx4_quantize");
+}
+
+extern "C" int swift_mx4_dequantize(void *w, int64_t ld_w, int dtype, const void *packed, int rows, int depth, int gated, void *stream) {
+    if (!packed || !w) return api_fail(SWIFT_EINVAL, "null argument");
+    if (int rc = check_matrix(rows, depth)) return rc;
+    if (!known_dtype(dtype)) return api_fail(SWIFT_EINVAL, "unknown dtype");
+    if (ld_w < depth) return api_fail(SWIFT_EINVAL, "rows overlap: a leading dimension is too small");
+    if (((uintptr_t)packed & 255) || !aligned(w, dtype))
+        return api_fail(SWIFT_EINVAL, "a pointer is not aligned to its elements (a packed matrix: to 256 bytes)");
+    Mx4DequantArgs a{matrix_at(packed, rows, depth, gated != 0), w, dtype, ld_w, rows, depth, gated ? TILE_GATEUP : TILE_PLAIN};
+    return device_status(launch_mx4_dequantize(a, (hipStream_t)stream), "swift_mx4_dequantize");
+}
+
+extern "C" int swift_mx4_linear(void *y, int64_t ld_y, int y_dtype, const void *x, int64_t ld_x, int x_dtype, int n, const void *packed, int rows,
+                                int depth, const void *residual, int64_t ld_residual, void *workspace, uint64_t workspace_bytes, void *stream) {
+    return product(EPI_LINEAR, Call{y, y_dtype, ld_y, x, x_dtype, ld_x, packed, rows, depth, n, residual, ld_residual, workspace, workspace_bytes}, stream);
+}
+
+extern "C" int swift_mx4_swiglu(void *h, int64_t ld_h, int h_dtype, const void *x, int64_t ld_x, int x_dtype, int n, const void *packed, int rows,
+                                int depth, void *workspace, uint64_t workspace_bytes, void *stream) {
+    return product(EPI_GATED, Call{h, h_dtype, ld_h, x, x_dtype, ld_x, packed, rows, depth, n, nullptr, 0, workspace, workspace_bytes}, stream);
+}

@@ -1,0 +1,206 @@
+// MXFP4 matrices: numbers to packed blocks and back, and activations to the B operand's layout (formats: swift_mx4.h).
+#include "swift_device.h"
+#include "swift_mx4.h"
+
+namespace swift {
+
+namespace {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// Row of the matrix in tile row j of row group rg, or -1: it comes from the other tensor (TILE_GATEUP).
+__device__ inline int tile_row(int mode, int part, int d, int rg, int j) {
+    if (mode == TILE_PLAIN) return 16 * rg + j;
+    if (mode == TILE_GATEUP) return (j >= 8) == (part == 1) ? 8 * rg + (j & 7) : -1;
+    const int gph = d >> 4, head = rg / gph, g = rg - head * gph;
+    return head * d + 8 * g + (j & 7) + (j >= 8 ? d >> 1 : 0);
+}
+
+// Elements k0 .. k0 + 7 of a row as fp32, zeros past K.  vec: the row allows 16-byte loads.
+template <typename T>
+__device__ inline void load8(const typename T::elem *row, int k0, int K, bool vec, float *v) {
+    if (vec && k0 + 8 <= K) {
+#pragma unroll
+        for (int i = 0; i < 8; i += T::VEC) T::unpack(*(const u32x4 *)(row + k0 + i), v + i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = k0 + i < K ? T::load1(row + k0 + i) : 0.f;
+    }
+}
+
+// One lane per block of 32.  The scale's exponent is that of the largest magnitude less two (its floor(log2) against the four of the largest
+// element's binade), at least -127; the conversion instruction divides by the scale, rounds to the nearest element, ties to the even
+// code, and saturates at 6, subnormals included.
+template <typename T>
+__global__ __launch_bounds__(256) void k_mx4_quantize(Mx4QuantArgs a, bool vec) {
+    const int S = mx4_tiles(a.K);
+    const int64_t n = (int64_t)a.n_rg * S * 64;
+    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < n; c += (int64_t)gridDim.x * 256) {
+        const int64_t piece = c >> 6;
+        const int lane = (int)(c & 63), rg = (int)(piece / S), s = (int)(piece - (int64_t)rg * S);
+        const int row = tile_row(a.mode, a.part, a.head_dim, rg, lane & 15), k0 = kMx4Tile * s + kMx4Block * (lane >> 4);
+        if (row < 0) continue;
+        u32x4 code = {0u, 0u, 0u, 0u};
+        uint32_t e = 0;
+        if (row < a.src_rows && k0 < a.K) {
+            const auto *src = (const typename T::elem *)a.src + (int64_t)row * a.ld;
+            float v[32];
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) load8<T>(src, k0 + i, a.K, vec, v + i);
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);  // (NaNs above infinity above numbers)
+            e = top >> 23;
+            if (e != 255) {
+                e = e > 2 ? e - 2 : 0;
+                const float scale = __uint_as_float(e << 23);  // (the instructions read its exponent field only: 0 is 2^-127)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    uint32_t q = 0;
+                    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[8 * w], v[8 * w + 1], scale, 0);
+                    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[8 * w + 2], v[8 * w + 3], scale, 1);
+                    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[8 * w + 4], v[8 * w + 5], scale, 2);
+                    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[8 * w + 6], v[8 * w + 7], scale, 3);
+                    code[w] = q;
+                }
+            }
+        }
+        ((u32x4 *)a.codes)[c] = code;
+        a.scales[c] = (uint8_t)e;
+    }
+}
+
+template <typename T>
+__device__ inline void store8(typename T::elem *row, int k0, int K, bool vec, const float *v) {
+    if (vec && k0 + 8 <= K) {
+        if constexpr (T::VEC == 8) {
+            u32x4 w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = (__float_as_uint(v[2 * i]) >> 16) | (__float_as_uint(v[2 * i + 1]) & 0xffff0000u);
+            *(u32x4 *)(row + k0) = w;
+        } else {
+            *(f32x4 *)(row + k0) = f32x4{v[0], v[1], v[2], v[3]};
+            *(f32x4 *)(row + k0 + 4) = f32x4{v[4], v[5], v[6], v[7]};
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (k0 + i < K) T::store1(row + k0 + i, v[i]);
+    }
+}
+
+// Eight codes as fp32 (every value is a bf16 number, subnormal ones included: nothing is rounded on the way out).
+__device__ inline void decode8(uint32_t w, float scale, float *v) {
+    const bf16x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t u = __builtin_bit_cast(uint32_t, p[i]);
+        v[2 * i] = __uint_as_float(u << 16);
+        v[2 * i + 1] = __uint_as_float(u & 0xffff0000u);
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_mx4_dequantize(Mx4DequantArgs a, bool vec) {
+    const int64_t n = (int64_t)a.w.n_rg * a.w.S * 64;
+    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < n; c += (int64_t)gridDim.x * 256) {
+        const int64_t piece = c >> 6;
+        const int lane = (int)(c & 63), j = lane & 15, rg = (int)(piece / a.w.S), s = (int)(piece - (int64_t)rg * a.w.S);
+        const int row = a.mode == TILE_GATEUP ? 8 * rg + (j & 7) : 16 * rg + j, k0 = kMx4Tile * s + kMx4Block * (lane >> 4);
+        if (row >= a.rows || k0 >= a.K) continue;
+        auto *dst = (typename T::elem *)a.dst + (int64_t)(a.mode == TILE_GATEUP && j >= 8 ? row + a.rows : row) * a.ld;
+        const u32x4 code = ((const u32x4 *)a.w.codes)[c];
+        const float scale = __uint_as_float((uint32_t)a.w.scales[c] << 23);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            float v[8];
+            decode8(code[w], scale, v);
+            store8<T>(dst, k0 + 8 * w, a.K, vec, v);
+        }
+    }
+}
+
+// v = hi + mid + lo exactly, for every finite v: hi is cut off, so that it never overflows.  Infinities and NaNs have one term.
+__device__ inline void split3_any(float v, uint32_t &hi, uint32_t &mid, uint32_t &lo) {
+    const uint32_t u = __float_as_uint(v);
+    hi = u >> 16;
+    mid = lo = 0;
+    if ((u & 0x7f800000u) == 0x7f800000u) {
+        if (u & 0x007fffffu) hi |= 0x40u;
+        return;
+    }
+    const float r = v - __uint_as_float(hi << 16);
+    mid = f32_to_bf16_rne_finite(r);
+    lo = f32_to_bf16_rne_finite(r - __uint_as_float(mid << 16));
+}
+
+// One thread per chunk of eight k and row.
+template <typename T>
+__global__ __launch_bounds__(256) void k_mx4_activations(Mx4ActArgs a, bool vec) {
+    constexpr int NT = T::VEC == 8 ? 1 : 3;
+    const int chunks = 16 * a.S, NC = NT * a.n;
+    const int64_t n = (int64_t)chunks * a.n;
+    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < n; c += (int64_t)gridDim.x * 256) {
+        const int r = (int)(c / chunks), ch = (int)(c - (int64_t)r * chunks);
+        float v[8];
+        load8<T>((const typename T::elem *)a.x + (int64_t)r * a.ld, 8 * ch, a.K, vec, v);
+        u32x4 t[3];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (NT == 1) {
+                t[0][i] = (__float_as_uint(v[2 * i]) >> 16) | (__float_as_uint(v[2 * i + 1]) & 0xffff0000u);
+            } else {
+                uint32_t h[2], m[2], l[2];
+                split3_any(v[2 * i], h[0], m[0], l[0]);
+                split3_any(v[2 * i + 1], h[1], m[1], l[1]);
+                t[0][i] = pack2(h[0], h[1]);
+                t[1][i] = pack2(m[0], m[1]);
+                t[2][i] = pack2(l[0], l[1]);
+            }
+        }
+        u32x4 *p = (u32x4 *)a.out + (int64_t)ch * NC + NT * r;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) p[i] = t[i];
+    }
+}
+
+unsigned grid_of(int64_t n) { return (unsigned)std::min<int64_t>((n + 255) / 256, 1 << 20); }
+bool rows_of_16_bytes(const void *p, int64_t ld, int dtype) {
+    const int eb = dtype == F32 ? 4 : 2;
+    return ((uintptr_t)p & 15) == 0 && (ld * eb & 15) == 0;
+}
+
+}  // namespace
+
+hipError_t launch_mx4_quantize(const Mx4QuantArgs &a, hipStream_t s) {
+    const bool vec = rows_of_16_bytes(a.src, a.ld, a.dtype);
+    const unsigned grid = grid_of((int64_t)a.n_rg * mx4_tiles(a.K) * 64);
+    if (a.dtype == F32)
+        hipLaunchKernelGGL(k_mx4_quantize<F32T>, dim3(grid), dim3(256), 0, s, a, vec);
+    else
+        hipLaunchKernelGGL(k_mx4_quantize<BF16T>, dim3(grid), dim3(256), 0, s, a, vec);
+    return hipGetLastError();
+}
+
+hipError_t launch_mx4_dequantize(const Mx4DequantArgs &a, hipStream_t s) {
+    const bool vec = rows_of_16_bytes(a.dst, a.ld, a.dtype);
+    const unsigned grid = grid_of((int64_t)a.w.n_rg * a.w.S * 64);
+    if (a.dtype == F32)
+        hipLaunchKernelGGL(k_mx4_dequantize<F32T>, dim3(grid), dim3(256), 0, s, a, vec);
+    else
+        hipLaunchKernelGGL(k_mx4_dequantize<BF16T>, dim3(grid), dim3(256), 0, s, a, vec);
+    return hipGetLastError();
+}
+
+hipError_t launch_mx4_activations(const Mx4ActArgs &a, hipStream_t s) {
+    const bool vec = rows_of_16_bytes(a.x, a.ld, a.dtype);
+    const unsigned grid = grid_of((int64_t)16 * a.S * a.n);
+    if (a.dtype == F32)
+        hipLaunchKernelGGL(k_mx4_activations<F32T>, dim3(grid), dim3(256), 0, s, a, vec);
+    else
+        hipLaunchKernelGGL(k_mx4_activations<BF16T>, dim3(grid), dim3(256), 0, s, a, vec);
+    return hipGetLastError();
+}
+
+}  // namespace swift

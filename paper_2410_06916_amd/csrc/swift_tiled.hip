@@ -173,112 +173,6 @@ hipError_t launch_embed_rows(const EmbedRowsArgs &a, const int32_t *tokens, hipS
 // ------------------------------------------------------------------------------------------
 // shared pieces of the projection kernels
 // ------------------------------------------------------------------------------------------
-// RMSNorm scale per block row from the producer's partial sums of squares.  A kernel requests the first 256 partials of its rows
-// (hidden <= 4096: all of them) ahead of its weights and adds them up once the weights are on their way: no branches
-// and no use of a loaded value in between (a partial past the last is the last one again, left out of the sum later), since a
-// wait there would hold the weights up.  The summation order is fixed.  One barrier, which orders LDS only, before the final sums.
-//
-// Up to 16 rows (row pitch 16): thread (q = t / 16, row r = t % 16) adds the partials q + 32 u in order of u, then 16 threads
-// add the 32 sums in order.
-struct NormPart {
-    float v[8];
-};
-__device__ inline NormPart mv_norm_load(const MvArgs &a, int p0 = 0) {
-    NormPart np;
-    const uint32_t at = threadIdx.x + 16 * p0, end = 16 * a.n_pss - 1;  // partial p of row r is word 16 p + r
-#pragma unroll
-    for (int u = 0; u < 8; ++u) np.v[u] = *(const float *)((const char *)a.pss + 4 * min(at + 512 * u, end));
-    return np;
-}
-__device__ inline void mv_norm_finish(const MvArgs &a, const NormPart &np, float *rs /* LDS [16] */, float *scratch /* LDS [512] */) {
-    const int tid = threadIdx.x, q = tid >> 4;
-    float ss = 0.f;
-#pragma unroll
-    for (int u = 0; u < 8; ++u) ss += q + 32 * u < a.n_pss ? np.v[u] : 0.f;
-    for (int p0 = 256; p0 < a.n_pss; p0 += 256) {
-        const NormPart more = mv_norm_load(a, p0);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) ss += p0 + q + 32 * u < a.n_pss ? more.v[u] : 0.f;
-    }
-    scratch[tid] = ss;
-    lds_barrier();
-    if (tid < 16) {
-        float t = 0.f;
-#pragma unroll
-        for (int q2 = 0; q2 < 32; ++q2) t += scratch[q2 * 16 + tid];
-        rs[tid] = 1.0f / sqrtf(t / (float)a.norm_dim + a.eps);
-    }
-    // (no barrier here: the scales are read by the epilogue only, and every caller has a barrier between
-    // this point and its epilogue)
-}
-
-// The same for exact layouts of 17..32 rows (row pitch 64), in the same order -- a row's scale must not depend on the rows it
-// shares a pass with: thread (row r, q) adds the partials q + 32 u and q + 16 + 32 u as two sums; then 32 threads add the 32 sums
-// in order.
-struct NormPart32 {
-    float v[2][8];
-};
-__device__ inline NormPart32 mv_norm32_load(const MvArgs &a, int p0 = 0) {
-    NormPart32 np;
-    const uint32_t r = threadIdx.x & 31, at = 64 * (p0 + (threadIdx.x >> 5)) + r, end = 64 * (a.n_pss - 1) + r;
-#pragma unroll
-    for (int half = 0; half < 2; ++half)
-#pragma unroll
-        for (int u = 0; u < 8; ++u) np.v[half][u] = *(const float *)((const char *)a.pss + 4 * min(at + 64 * (16 * half + 32 * u), end));
-    return np;
-}
-__device__ inline void mv_norm32_finish(const MvArgs &a, const NormPart32 &np, float *rs /* LDS [32] */, float *scratch /* LDS [1024] */) {
-    const int tid = threadIdx.x, r = tid & 31, q0 = tid >> 5;
-    float ss[2] = {0.f, 0.f};
-    auto add = [&](int p0, const NormPart32 &n) {
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-            for (int u = 0; u < 8; ++u) ss[half] += p0 + q0 + 16 * half + 32 * u < a.n_pss ? n.v[half][u] : 0.f;
-    };
-    add(0, np);
-    for (int p0 = 256; p0 < a.n_pss; p0 += 256) add(p0, mv_norm32_load(a, p0));
-    scratch[q0 * 32 + r] = ss[0];
-    scratch[(q0 + 16) * 32 + r] = ss[1];
-    lds_barrier();
-    if (tid < 32) {
-        float t = 0.f;
-#pragma unroll
-        for (int q2 = 0; q2 < 32; ++q2) t += scratch[q2 * 32 + tid];
-        rs[tid] = 1.0f / sqrtf(t / (float)a.norm_dim + a.eps);
-    }
-}
-
-// The same for bulk layouts of 64 rows: thread = (partial p mod 8, row r), then 64 threads add the 8 per-thread sums in order.
-struct NormPart64 {
-    float v[32];
-};
-__device__ inline NormPart64 mv_norm64_load(const MvArgs &a, int p0 = 0) {
-    NormPart64 np;
-    const uint32_t at = threadIdx.x + 64 * p0, end = 64 * (a.n_pss - 1) + (threadIdx.x & 63);  // partial p of row r is word 64 p + r
-#pragma unroll
-    for (int u = 0; u < 32; ++u) np.v[u] = *(const float *)((const char *)a.pss + 4 * min(at + 512 * u, end));
-    return np;
-}
-__device__ inline void mv_norm64_finish(const MvArgs &a, const NormPart64 &np, float *rs /* LDS [64] */, float *scratch /* LDS [512] */) {
-    const int tid = threadIdx.x, q = tid >> 6;
-    float ss = 0.f;
-    auto add = [&](int p0, const NormPart64 &n) {
-#pragma unroll
-        for (int u = 0; u < 32; ++u) ss += p0 + q + 8 * u < a.n_pss ? n.v[u] : 0.f;
-    };
-    add(0, np);
-    for (int p0 = 256; p0 < a.n_pss; p0 += 256) add(p0, mv_norm64_load(a, p0));
-    scratch[tid] = ss;
-    lds_barrier();
-    if (tid < 64) {
-        float t = 0.f;
-#pragma unroll
-        for (int q2 = 0; q2 < 8; ++q2) t += scratch[q2 * 64 + tid];
-        rs[tid] = 1.0f / sqrtf(t / (float)a.norm_dim + a.eps);
-    }
-}
-
 // Slices (of the 8 K slices of a row group) whose sums are added first, in slice order, before the
 // group sums are added in group order: 8, 4, 2 or 1.  It is the number of slices one workgroup of
 // the block kernel covers when that kernel splits K over workgroups to fill the chip, and it
