@@ -147,10 +147,11 @@ Layout make_layout(const swift_model_config &c) {
     const uint64_t subs = L.tiled ? kMacroSub : 1;
     L.sub_x = kMaxBlockRows * H;
     L.sub_q = kMaxBlockRows * Q;
-    // (64 rows of two terms; exact layouts of three terms have up to 32 rows)
-    L.sub_xs = ceil_div(H, 32) * 4 * 2 * kMaxBlockRows * 8;
-    L.sub_as = ceil_div(Q, 32) * 4 * 2 * kMaxBlockRows * 8;
-    L.sub_hs = ceil_div(F, 32) * 4 * 2 * kMaxBlockRows * 8;
+    // (64 rows of two terms; exact layouts of three terms have up to 32 rows.  MXFP4: whole super-tiles, see mx4_act_tiles)
+    auto split_elems = [&](uint64_t K) { return (L.mx4 ? (uint64_t)mx4_act_tiles((int)K) * kMx4Tile : ceil_div(K, 32) * 32) * 2 * kMaxBlockRows; };
+    L.sub_xs = split_elems(H);
+    L.sub_as = split_elems(Q);
+    L.sub_hs = split_elems(F);
     L.sub_pss = ceil_div(H, 16) * kMaxBlockRows;
     L.x = take(subs * L.sub_x * 4);
     L.q = take(subs * L.sub_q * 4);
@@ -639,9 +640,9 @@ int forward_block_tiled(swift_ctx *x, const int32_t *tokens, int R, int pos0, co
         if (L.mx4 && epi != EPI_LOGITS) {
             const int all = kc == SWIFT_KC_QKV ? (Q + 2 * KV) / 16 : m.n_rg;
             const auto *codes = (const uint8_t *)(const void *)m.Wt;
-            const Mx4Matrix w{codes, codes + mx4_code_bytes(all, m.K), mx4_tiles(m.K), all};
+            const Mx4Matrix w{codes, codes + mx4_code_bytes(all, m.K), m.K, mx4_tiles(m.K), all};
             HIP_TRY(timed(x, kc, weight_bytes(c.dtype, m.O - 16 * rg0, m.K), [&] {
-                return macro ? launch_mx4_macro(epi, m, ma, w, rg0, s) : launch_mx4_mv(epi, m, w, rg0, s);
+                return macro ? launch_mx4_macro(epi, m, ma, w, rg0, x->n_cu, s) : launch_mx4_mv(epi, m, w, rg0, s);
             }));
         } else if (macro) {
             HIP_TRY(timed(x, kc, (uint64_t)m.O * m.K * 2, [&] { return launch_gemm(epi, m, ma, x->n_cu, x->gemm_rgw, s); }));
@@ -1014,6 +1015,8 @@ extern "C" int swift_create(const swift_model_config *cfg, void *device_mem, uin
         }
     }
     e = hipMemsetAsync(x->base + L.mv_counters, 0, 4096 * 4, x->stream);
+    // (what lies past a depth that is no whole number of super-tiles has to be zeros, and is written by nobody)
+    if (e == hipSuccess && L.mx4) e = hipMemsetAsync(x->base + L.xs, 0, L.pss - L.xs, x->stream);
     if (e == hipSuccess) e = hipMemcpyAsync(x->base + L.cos, ct.data(), ct.size() * 4, hipMemcpyHostToDevice, x->stream);
     if (e == hipSuccess) e = hipMemcpyAsync(x->base + L.sin, stb.data(), stb.size() * 4, hipMemcpyHostToDevice, x->stream);
     if (e == hipSuccess) e = hipStreamSynchronize(x->stream);

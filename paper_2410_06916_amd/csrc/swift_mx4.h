@@ -27,7 +27,7 @@ inline uint64_t mx4_scale_bytes(uint64_t n_rg, int K) { return n_rg * mx4_tiles(
 
 struct Mx4Matrix {
     const uint8_t *codes, *scales;
-    int S;      // super-tiles of a row group
+    int K, S;   // depth, super-tiles of a row group
     int n_rg;   // row groups
 };
 
@@ -51,19 +51,23 @@ struct Mx4DequantArgs {
 };
 hipError_t launch_mx4_dequantize(const Mx4DequantArgs &a, hipStream_t s);
 
-// Activations [n][K] to the B operand's layout [16 S chunks][NC columns][8 k] bf16, zeros past K: a bf16 row is one column, an fp32 row
-// three (value = hi + mid + lo; column 3 r + term).
+// Super-tiles of activations that the blocked product reads: its pipeline has at least two.
+__host__ __device__ inline int mx4_act_tiles(int K) { return K > kMx4Tile ? mx4_tiles(K) : 2; }
+// Activations [n][K] to the B operand's layout, in sub-blocks of `per` rows: [sub-block][16 S chunks][pitch columns][8 k] bf16, zeros past
+// K; a bf16 row is one column, an fp32 row three (value = hi + mid + lo; column 3 r + term).  Columns of rows that do not exist
+// are left as they are.
 inline int mx4_terms(int dtype) { return dtype == F32 ? 3 : 1; }
 struct Mx4ActArgs {
     const void *x;
     int dtype;
     int64_t ld;
     int n, K, S;
+    int per, pitch;
     uint16_t *out;
 };
 hipError_t launch_mx4_activations(const Mx4ActArgs &a, hipStream_t s);
 
-// ---- products (swift_mx4.hip)
+// ---- products (swift_mx4.hip; blocked: swift_mx4_gemm.hip)
 // What follows the dot products of a call that is not part of a model's pass, beside Epilogue's.
 enum Mx4Epilogue : int {
     EPI_LINEAR = 8,  // y = W x (+ residual)
@@ -81,10 +85,8 @@ constexpr int kMx4MaxColumns = 128;
 
 // A model's projection (epilogue: EPI_QKV, EPI_RESID or EPI_SWIGLU) of a block of a.R rows, as launch_mv, over the row groups [rg0, a.n_rg) of w.
 hipError_t launch_mx4_mv(int epilogue, const MvArgs &a, const Mx4Matrix &w, int rg0, hipStream_t s);
-// The same for a prompt macro block, as launch_gemm.
-hipError_t launch_mx4_macro(int epilogue, const MvArgs &a, const MacroArgs &ma, const Mx4Matrix &w, int rg0, hipStream_t s);
-// A call's product: n rows (columns as launch_mx4_activations lays them out, at most kMx4MaxColumns) against w, O results a row
-// (EPI_GATED: of the gate and the up half each).
+// A call's product: n rows as launch_mx4_activations lays them out (one sub-block, pitched for its own columns, at most
+// kMx4MaxColumns) against w, O results a row (EPI_GATED: of the gate and the up half each).
 struct Mx4CallArgs {
     Mx4Matrix w;
     const uint16_t *x;
@@ -92,5 +94,11 @@ struct Mx4CallArgs {
     Mx4Out out;
 };
 hipError_t launch_mx4_call(int epilogue, const Mx4CallArgs &a, hipStream_t s);
+
+// A prompt macro block of a model, as launch_gemm, over the row groups [rg0, a.n_rg) of w.  The activations of a sub-block are
+// mx4_act_tiles(K) super-tiles, zeros past K.
+hipError_t launch_mx4_macro(int epilogue, const MvArgs &a, const MacroArgs &ma, const Mx4Matrix &w, int rg0, int n_cu, hipStream_t s);
+// A call's product of any number of rows, in sub-blocks of 128 / terms rows and 128 columns, mx4_act_tiles(K) super-tiles each.
+hipError_t launch_mx4_call_blocked(int epilogue, const Mx4CallArgs &a, int n_cu, hipStream_t s);
 
 }  // namespace swift

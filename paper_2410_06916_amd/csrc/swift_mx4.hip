@@ -5,50 +5,11 @@
 #include "swift_device.h"
 #include "swift_mv.h"
 #include "swift_mx4.h"
+#include "swift_mx4_device.h"
 
 namespace swift {
 
 namespace {
-
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
-// Eight codes to the eight bf16 values they stand for (exact): an A operand.
-__device__ inline bf16x8 mx4_decode(uint32_t w, float scale) {
-    const bf16x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
-    const bf16x2 p2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
-    return bf16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
-}
-
-__device__ inline float load_as_f32(const void *p, int dtype, int64_t i) {
-    return dtype == F32 ? ((const float *)p)[i] : BF16T::load1((const uint16_t *)p + i);
-}
-__device__ inline void store_f32_as(void *p, int dtype, int64_t i, float v) {
-    if (dtype == F32)
-        ((float *)p)[i] = v;
-    else
-        ((uint16_t *)p)[i] = f32_to_bf16_rne(v);  // (the result's one rounding)
-}
-
-// What follows the dot products of one row group of a call, by thread t of `threads`.  Y(r, j): row r's product with tile row j.
-template <int EPI, typename YF>
-__device__ inline void mx4_call_epilogue(const Mx4Out &o, int R, int O, int rg, int t, int threads, YF Y) {
-    if (EPI == EPI_LINEAR) {
-        for (int i = t; i < 16 * R; i += threads) {
-            const int r = i >> 4, row = 16 * rg + (i & 15);
-            if (row >= O) continue;
-            float y = Y(r, i & 15);
-            if (o.residual) y += load_as_f32(o.residual, o.dtype, r * o.ld_res + row);
-            store_f32_as(o.y, o.dtype, r * o.ld + row, y);
-        }
-    } else {
-        for (int i = t; i < 8 * R; i += threads) {
-            const int r = i >> 3, j = i & 7, row = 8 * rg + j;
-            if (row >= O) continue;
-            const float g = Y(r, j), u = Y(r, j + 8);
-            store_f32_as(o.y, o.dtype, r * o.ld + row, g / (1.0f + expf(-g)) * u);
-        }
-    }
-}
 
 // Up to 128 columns: a workgroup per row group, its 8 wavefronts a slice of the super-tiles each.  A column's result is the sum of its slices
 // in order, a row's the sum of its terms' in order, so it does not depend on the rows that share the launch.
@@ -145,24 +106,6 @@ hipError_t launch_mx4_mv(int epi, const MvArgs &a, const Mx4Matrix &w, int rg0, 
         case EPI_SWIGLU: return launch_mx4_mv_e<EPI_SWIGLU>(w, a, Mx4Out{}, rg0, NT, NC, s);
     }
     return hipErrorInvalidValue;
-}
-
-hipError_t launch_mx4_macro(int epi, const MvArgs &a, const MacroArgs &ma, const Mx4Matrix &w, int rg0, hipStream_t s) {
-    if (ma.S < 1 || ma.S > kMacroSub || ma.rows_last < 1 || ma.rows_last > 64 || a.RL != (64 | kBulkLayout) || a.rp != 64 || a.tree || a.q_s)
-        return hipErrorInvalidValue;
-    for (int sb = 0; sb < ma.S; ++sb) {
-        MvArgs m = a;
-        m.R = sb == ma.S - 1 ? ma.rows_last : 64;
-        m.pos0 = a.pos0 + 64 * sb;
-        m.in_s = a.in_s + (size_t)sb * ma.in_s;
-        if (a.pss) m.pss = a.pss + (size_t)sb * ma.pss;
-        if (a.out_f32) m.out_f32 = a.out_f32 + (size_t)sb * ma.out_f32;
-        if (a.out_s) m.out_s = a.out_s + (size_t)sb * ma.out_s;
-        if (a.pss_out) m.pss_out = a.pss_out + (size_t)sb * ma.pss_out;
-        const hipError_t e = launch_mx4_mv(epi, m, w, rg0, s);
-        if (e != hipSuccess) return e;
-    }
-    return hipSuccess;
 }
 
 hipError_t launch_mx4_call(int epi, const Mx4CallArgs &c, hipStream_t s) {

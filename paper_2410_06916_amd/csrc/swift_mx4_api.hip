@@ -1,5 +1,6 @@
 // C-ABI layer of the MXFP4 operators (declared in include/swift.h): checks of arguments, sizes, and the launches a call is made of.
 #include <algorithm>
+#include <atomic>
 
 #include "swift_mx4.h"
 
@@ -25,13 +26,32 @@ int row_groups(int rows, bool gated) { return gated ? (rows + 7) / 8 : (rows + 1
 Mx4Matrix matrix_at(const void *packed, int rows, int depth, bool gated) {
     const int n_rg = row_groups(rows, gated);
     const auto *codes = (const uint8_t *)packed;
-    return Mx4Matrix{codes, codes + mx4_code_bytes(n_rg, depth), mx4_tiles(depth), n_rg};
+    return Mx4Matrix{codes, codes + mx4_code_bytes(n_rg, depth), depth, mx4_tiles(depth), n_rg};
 }
 
-// Rows of x that one launch takes.
-int launch_rows(int x_dtype) { return kMx4MaxColumns / mx4_terms(x_dtype); }
+int compute_units() {
+    static std::atomic<int> known[64];
+    int dev = 0, n = 0;
+    if (hipGetDevice(&dev) != hipSuccess) return 256;
+    std::atomic<int> *at = dev >= 0 && dev < 64 ? &known[dev] : nullptr;
+    if (at && (n = at->load(std::memory_order_relaxed)) > 0) return n;
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1) n = 256;
+    if (at) at->store(n, std::memory_order_relaxed);
+    return n;
+}
+
+// Up to this many columns a product goes through the kernel that reads every weight once for all rows, beyond through the blocked one.
+constexpr int kFewColumns = 96;
+// Rows of a blocked launch (a multiple of both sub-block heights): bounds the workspace.
+constexpr int kBlockedRows = 128 * 42;
+
+bool few(int n, int x_dtype) { return n * mx4_terms(x_dtype) <= kFewColumns; }
 uint64_t workspace(int depth, int n, int x_dtype) {
-    return (uint64_t)mx4_tiles(depth) * kMx4Tile * mx4_terms(x_dtype) * std::min(n, launch_rows(x_dtype)) * 2;
+    const uint64_t terms = mx4_terms(x_dtype);
+    if (few(n, x_dtype)) return (uint64_t)mx4_tiles(depth) * kMx4Tile * 2 * terms * n;
+    const uint64_t k = (uint64_t)mx4_act_tiles(depth) * kMx4Tile * 2;
+    const int per = 128 / (int)terms, rows = std::min(n, kBlockedRows);
+    return k * 128 * ((rows + per - 1) / per);
 }
 
 struct Call {
@@ -62,18 +82,21 @@ int product(int epi, const Call &c, void *stream) {
     if (!c.ws || ((uintptr_t)c.ws & 255) || c.ws_bytes < need)
         return api_fail(SWIFT_ECAPACITY, "the workspace is missing, not aligned to 256 bytes, or smaller than swift_mx4_workspace says");
     const auto s = (hipStream_t)stream;
-    const int per = launch_rows(c.x_dtype), xb = c.x_dtype == SWIFT_F32 ? 4 : 2, yb = c.y_dtype == SWIFT_F32 ? 4 : 2;
+    const int terms = mx4_terms(c.x_dtype), xb = c.x_dtype == SWIFT_F32 ? 4 : 2, yb = c.y_dtype == SWIFT_F32 ? 4 : 2;
+    const bool blocked = !few(c.n, c.x_dtype);
     Mx4CallArgs a{};
     a.w = matrix_at(c.packed, c.rows, c.depth, epi == EPI_GATED);
     a.x = (const uint16_t *)c.ws;
-    a.terms = mx4_terms(c.x_dtype);
+    a.terms = terms;
     a.O = c.rows;
-    for (int r0 = 0; r0 < c.n; r0 += per) {
-        a.n = std::min(per, c.n - r0);
-        Mx4ActArgs act{(const char *)c.x + r0 * c.ld_x * xb, c.x_dtype, c.ld_x, a.n, c.depth, a.w.S, (uint16_t *)c.ws};
+    for (int r0 = 0; r0 < c.n; r0 += kBlockedRows) {
+        a.n = std::min(kBlockedRows, c.n - r0);
+        Mx4ActArgs act{(const char *)c.x + r0 * c.ld_x * xb, c.x_dtype, c.ld_x, a.n, c.depth, blocked ? mx4_act_tiles(c.depth) : a.w.S, blocked ? 128 / terms : a.n, blocked ? 128 : terms * a.n,
+                       (uint16_t *)c.ws};
         if (int rc = device_status(launch_mx4_activations(act, s), "activations of an MXFP4 product")) return rc;
         a.out = Mx4Out{(char *)c.y + r0 * c.ld_y * yb, c.y_dtype, c.ld_y, c.residual ? (const char *)c.residual + r0 * c.ld_res * yb : nullptr, c.ld_res};
-        if (int rc = device_status(launch_mx4_call(epi, a, s), "MXFP4 product")) return rc;
+        const hipError_t e = blocked ? launch_mx4_call_blocked(epi, a, compute_units(), s) : launch_mx4_call(epi, a, s);
+        if (int rc = device_status(e, "MXFP4 product")) return rc;
     }
     return SWIFT_OK;
 }

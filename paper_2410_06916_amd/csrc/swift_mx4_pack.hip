@@ -1,12 +1,13 @@
 // MXFP4 matrices: numbers to packed blocks and back, and activations to the B operand's layout (formats: swift_mx4.h).
+#include <algorithm>
+
 #include "swift_device.h"
 #include "swift_mx4.h"
+#include "swift_mx4_device.h"
 
 namespace swift {
 
 namespace {
-
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // Row of the matrix in tile row j of row group rg, or -1: it comes from the other tensor (TILE_GATEUP).
 __device__ inline int tile_row(int mode, int part, int d, int rg, int j) {
@@ -90,16 +91,7 @@ __device__ inline void store8(typename T::elem *row, int k0, int K, bool vec, co
 }
 
 // Eight codes as fp32 (every value is a bf16 number, subnormal ones included: nothing is rounded on the way out).
-__device__ inline void decode8(uint32_t w, float scale, float *v) {
-    const bf16x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1),
-                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3)};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t u = __builtin_bit_cast(uint32_t, p[i]);
-        v[2 * i] = __uint_as_float(u << 16);
-        v[2 * i + 1] = __uint_as_float(u & 0xffff0000u);
-    }
-}
+__device__ inline void decode8(uint32_t w, float scale, float *v) { BF16T::unpack(__builtin_bit_cast(u32x4, mx4_decode(w, scale)), v); }
 
 template <typename T>
 __global__ __launch_bounds__(256) void k_mx4_dequantize(Mx4DequantArgs a, bool vec) {
@@ -135,34 +127,43 @@ __device__ inline void split3_any(float v, uint32_t &hi, uint32_t &mid, uint32_t
     lo = f32_to_bf16_rne_finite(r - __uint_as_float(mid << 16));
 }
 
-// One thread per chunk of eight k and row.
+// A workgroup turns 64 rows (at most) of a sub-block by 16 chunks through LDS: rows are read 128 k at a time, columns are written a KB at a
+// time.  (A thread per chunk that writes where its chunk goes: 512 rows of 4096 bf16 7.5 us.)
+constexpr int kActRows = 64;
 template <typename T>
-__global__ __launch_bounds__(256) void k_mx4_activations(Mx4ActArgs a, bool vec) {
-    constexpr int NT = T::VEC == 8 ? 1 : 3;
-    const int chunks = 16 * a.S, NC = NT * a.n;
-    const int64_t n = (int64_t)chunks * a.n;
-    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < n; c += (int64_t)gridDim.x * 256) {
-        const int r = (int)(c / chunks), ch = (int)(c - (int64_t)r * chunks);
+__global__ __launch_bounds__(256) void k_mx4_activations(Mx4ActArgs a, int blocks_of_sub, bool vec) {
+    constexpr int NT = T::VEC == 8 ? 1 : 3, P = kActRows * NT + 1;
+    __shared__ u32x4 turn[16 * P];
+    const int s = blockIdx.x, sub = blockIdx.y / blocks_of_sub, b = blockIdx.y - sub * blocks_of_sub;
+    const int r0 = sub * a.per + b * kActRows, rows = min(kActRows, min(a.per - b * kActRows, a.n - r0));
+    if (rows <= 0) return;
+    for (int i = threadIdx.x; i < 16 * rows; i += 256) {
+        const int r = i >> 4, ch = i & 15;
         float v[8];
-        load8<T>((const typename T::elem *)a.x + (int64_t)r * a.ld, 8 * ch, a.K, vec, v);
+        load8<T>((const typename T::elem *)a.x + (int64_t)(r0 + r) * a.ld, kMx4Tile * s + 8 * ch, a.K, vec, v);
         u32x4 t[3];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int j = 0; j < 4; ++j) {
             if constexpr (NT == 1) {
-                t[0][i] = (__float_as_uint(v[2 * i]) >> 16) | (__float_as_uint(v[2 * i + 1]) & 0xffff0000u);
+                t[0][j] = (__float_as_uint(v[2 * j]) >> 16) | (__float_as_uint(v[2 * j + 1]) & 0xffff0000u);
             } else {
                 uint32_t h[2], m[2], l[2];
-                split3_any(v[2 * i], h[0], m[0], l[0]);
-                split3_any(v[2 * i + 1], h[1], m[1], l[1]);
-                t[0][i] = pack2(h[0], h[1]);
-                t[1][i] = pack2(m[0], m[1]);
-                t[2][i] = pack2(l[0], l[1]);
+                split3_any(v[2 * j], h[0], m[0], l[0]);
+                split3_any(v[2 * j + 1], h[1], m[1], l[1]);
+                t[0][j] = pack2(h[0], h[1]);
+                t[1][j] = pack2(m[0], m[1]);
+                t[2][j] = pack2(l[0], l[1]);
             }
         }
-        u32x4 *p = (u32x4 *)a.out + (int64_t)ch * NC + NT * r;
 #pragma unroll
-        for (int i = 0; i < NT; ++i) p[i] = t[i];
+        for (int j = 0; j < NT; ++j) turn[ch * P + NT * r + j] = t[j];
     }
+    __syncthreads();
+    const int cols = NT * rows;
+    u32x4 *out = (u32x4 *)a.out + ((int64_t)sub * a.S + s) * 16 * a.pitch + NT * b * kActRows;
+    const int lane = threadIdx.x & 63;
+    for (int ch = threadIdx.x >> 6; ch < 16; ch += 4)
+        for (int c = lane; c < cols; c += 64) out[(int64_t)ch * a.pitch + c] = turn[ch * P + c];
 }
 
 unsigned grid_of(int64_t n) { return (unsigned)std::min<int64_t>((n + 255) / 256, 1 << 20); }
@@ -195,11 +196,12 @@ hipError_t launch_mx4_dequantize(const Mx4DequantArgs &a, hipStream_t s) {
 
 hipError_t launch_mx4_activations(const Mx4ActArgs &a, hipStream_t s) {
     const bool vec = rows_of_16_bytes(a.x, a.ld, a.dtype);
-    const unsigned grid = grid_of((int64_t)16 * a.S * a.n);
+    const int per_sub = (std::min(a.per, a.n) + kActRows - 1) / kActRows;
+    const dim3 grid((unsigned)a.S, (unsigned)((a.n + a.per - 1) / a.per * per_sub));
     if (a.dtype == F32)
-        hipLaunchKernelGGL(k_mx4_activations<F32T>, dim3(grid), dim3(256), 0, s, a, vec);
+        hipLaunchKernelGGL(k_mx4_activations<F32T>, grid, dim3(256), 0, s, a, per_sub, vec);
     else
-        hipLaunchKernelGGL(k_mx4_activations<BF16T>, dim3(grid), dim3(256), 0, s, a, vec);
+        hipLaunchKernelGGL(k_mx4_activations<BF16T>, grid, dim3(256), 0, s, a, per_sub, vec);
     return hipGetLastError();
 }
 
