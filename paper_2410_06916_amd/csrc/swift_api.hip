@@ -642,7 +642,7 @@ int forward_block_tiled(swift_ctx *x, const int32_t *tokens, int R, int pos0, co
             const auto *codes = (const uint8_t *)(const void *)m.Wt;
             const Mx4Matrix w{codes, codes + mx4_code_bytes(all, m.K), m.K, mx4_tiles(m.K), all};
             HIP_TRY(timed(x, kc, weight_bytes(c.dtype, m.O - 16 * rg0, m.K), [&] {
-                return macro ? launch_mx4_macro(epi, m, ma, w, rg0, x->n_cu, s) : launch_mx4_mv(epi, m, w, rg0, s);
+                return macro ? launch_mx4_macro(epi, m, ma, w, rg0, x->n_cu, s) : launch_mx4_mv(epi, m, w, rg0, x->n_cu, s);
             }));
         } else if (macro) {
             HIP_TRY(timed(x, kc, (uint64_t)m.O * m.K * 2, [&] { return launch_gemm(epi, m, ma, x->n_cu, x->gemm_rgw, s); }));

@@ -84,16 +84,31 @@ struct Mx4Out {
 constexpr int kMx4MaxColumns = 128;
 
 // A model's projection (epilogue: EPI_QKV, EPI_RESID or EPI_SWIGLU) of a block of a.R rows, as launch_mv, over the row groups [rg0, a.n_rg) of w.
-hipError_t launch_mx4_mv(int epilogue, const MvArgs &a, const Mx4Matrix &w, int rg0, hipStream_t s);
-// A call's product: n rows as launch_mx4_activations lays them out (one sub-block, pitched for its own columns, at most
-// kMx4MaxColumns) against w, O results a row (EPI_GATED: of the gate and the up half each).
+hipError_t launch_mx4_mv(int epilogue, const MvArgs &a, const Mx4Matrix &w, int rg0, int n_cu, hipStream_t s);
+// A call's product: n rows (at most kMx4MaxColumns columns) against w, O results a row (EPI_GATED: of the gate and the up half each).
+// The rows: as launch_mx4_activations lays them out (one sub-block, pitched for its own columns); or as the caller has them, bf16 (direct:
+// rows of 16-byte units, mx4_rows_direct) or fp32 (x32: mx4_rows_x32), ld_x elements apart.
 struct Mx4CallArgs {
     Mx4Matrix w;
     const uint16_t *x;
     int n, terms, O;
     Mx4Out out;
+    bool direct;
+    const float *x32;
+    int64_t ld_x;
 };
-hipError_t launch_mx4_call(int epilogue, const Mx4CallArgs &a, hipStream_t s);
+// LDS that the eight slices of B take there: each 16 bytes of zeros and its lines (columns chunk by chunk, chunk_bytes a chunk), 16 bytes apart.
+__host__ __device__ inline uint32_t mx4_lds_line(int slice_tiles, uint32_t chunk_bytes) { return 16u * slice_tiles * chunk_bytes + 16; }
+inline size_t mx4_lds_bytes(int K, int lines, int chunk_bytes) { return 8 * (16 + (size_t)lines * mx4_lds_line((mx4_tiles(K) + 7) / 8, chunk_bytes)); }
+constexpr size_t kMx4LdsMost = 96 * 1024;
+// (few enough for one column block, and for LDS: more rows are read more often, and are worth laying out first)
+inline bool mx4_rows_direct(const void *x, int dtype, int64_t ld, int n, int K) {
+    return dtype == BF16 && ((uintptr_t)x & 15) == 0 && (K & 7) == 0 && n <= 16 && (n == 1 || ((ld & 7) == 0 && ld < 1 << 24)) &&
+           mx4_lds_bytes(K, n, 16) <= kMx4LdsMost;
+}
+// (three columns a row in one column block, and their terms in LDS)
+inline bool mx4_rows_x32(int dtype, int n, int K) { return dtype == F32 && n <= 5 && mx4_lds_bytes(K, 1, 48 * n) <= kMx4LdsMost; }
+hipError_t launch_mx4_call(int epilogue, const Mx4CallArgs &a, int n_cu, hipStream_t s);
 
 // A prompt macro block of a model, as launch_gemm, over the row groups [rg0, a.n_rg) of w.  The activations of a sub-block are
 // mx4_act_tiles(K) super-tiles, zeros past K.

@@ -48,6 +48,7 @@ constexpr int kBlockedRows = 128 * 42;
 bool few(int n, int x_dtype) { return n * mx4_terms(x_dtype) <= kFewColumns; }
 uint64_t workspace(int depth, int n, int x_dtype) {
     const uint64_t terms = mx4_terms(x_dtype);
+    if (mx4_rows_x32(x_dtype, n, depth)) return 0;
     if (few(n, x_dtype)) return (uint64_t)mx4_tiles(depth) * kMx4Tile * 2 * terms * n;
     const uint64_t k = (uint64_t)mx4_act_tiles(depth) * kMx4Tile * 2;
     const int per = 128 / (int)terms, rows = std::min(n, kBlockedRows);
@@ -79,7 +80,7 @@ int product(int epi, const Call &c, void *stream) {
     if (!aligned(c.x, c.x_dtype) || !aligned(c.y, c.y_dtype) || (c.residual && !aligned(c.residual, c.y_dtype)) || ((uintptr_t)c.packed & 255))
         return api_fail(SWIFT_EINVAL, "a pointer is not aligned to its elements (a packed matrix: to 256 bytes)");
     const uint64_t need = workspace(c.depth, c.n, c.x_dtype);
-    if (!c.ws || ((uintptr_t)c.ws & 255) || c.ws_bytes < need)
+    if (need && (!c.ws || ((uintptr_t)c.ws & 255) || c.ws_bytes < need))
         return api_fail(SWIFT_ECAPACITY, "the workspace is missing, not aligned to 256 bytes, or smaller than swift_mx4_workspace says");
     const auto s = (hipStream_t)stream;
     const int terms = mx4_terms(c.x_dtype), xb = c.x_dtype == SWIFT_F32 ? 4 : 2, yb = c.y_dtype == SWIFT_F32 ? 4 : 2;
@@ -89,13 +90,22 @@ int product(int epi, const Call &c, void *stream) {
     a.x = (const uint16_t *)c.ws;
     a.terms = terms;
     a.O = c.rows;
+    if (!blocked && (mx4_rows_x32(c.x_dtype, c.n, c.depth) || mx4_rows_direct(c.x, c.x_dtype, c.ld_x, c.n, c.depth))) {
+        a.n = c.n;
+        a.direct = c.x_dtype == SWIFT_BF16;
+        a.x = a.direct ? (const uint16_t *)c.x : nullptr;
+        a.x32 = a.direct ? nullptr : (const float *)c.x;
+        a.ld_x = c.ld_x;
+        a.out = Mx4Out{c.y, c.y_dtype, c.ld_y, c.residual, c.ld_res};
+        return device_status(launch_mx4_call(epi, a, compute_units(), s), "MXFP4 product");
+    }
     for (int r0 = 0; r0 < c.n; r0 += kBlockedRows) {
         a.n = std::min(kBlockedRows, c.n - r0);
         Mx4ActArgs act{(const char *)c.x + r0 * c.ld_x * xb, c.x_dtype, c.ld_x, a.n, c.depth, blocked ? mx4_act_tiles(c.depth) : a.w.S, blocked ? 128 / terms : a.n, blocked ? 128 : terms * a.n,
                        (uint16_t *)c.ws};
         if (int rc = device_status(launch_mx4_activations(act, s), "activations of an MXFP4 product")) return rc;
         a.out = Mx4Out{(char *)c.y + r0 * c.ld_y * yb, c.y_dtype, c.ld_y, c.residual ? (const char *)c.residual + r0 * c.ld_res * yb : nullptr, c.ld_res};
-        const hipError_t e = blocked ? launch_mx4_call_blocked(epi, a, compute_units(), s) : launch_mx4_call(epi, a, s);
+        const hipError_t e = blocked ? launch_mx4_call_blocked(epi, a, compute_units(), s) : launch_mx4_call(epi, a, compute_units(), s);
         if (int rc = device_status(e, "MXFP4 product")) return rc;
     }
     return SWIFT_OK;

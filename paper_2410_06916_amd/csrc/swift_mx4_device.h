@@ -2,10 +2,23 @@
 #pragma once
 #include <math.h>
 
+#include <type_traits>
+#include <utility>
+
 #include "swift_device.h"
 #include "swift_mx4.h"
 
 namespace swift {
+
+// f(0), f(1), .. f(N - 1), each a constant.
+template <int N, typename F, int... I>
+__device__ inline void each_of(F &&f, std::integer_sequence<int, I...>) {
+    (f(std::integral_constant<int, I>()), ...);
+}
+template <int N, typename F>
+__device__ inline void each(F &&f) {
+    each_of<N>(f, std::make_integer_sequence<int, N>());
+}
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
@@ -14,6 +27,45 @@ __device__ inline bf16x8 mx4_decode(uint32_t w, float scale) {
     const bf16x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
     const bf16x2 p2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
     return bf16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+}
+
+// Elements k0 .. k0 + 7 of a row as fp32, zeros past K.  vec: the row allows 16-byte loads.
+template <typename T>
+__device__ inline void mx4_load8(const typename T::elem *row, int k0, int K, bool vec, float *v) {
+    if (vec && k0 + 8 <= K) {
+#pragma unroll
+        for (int i = 0; i < 8; i += T::VEC) T::unpack(*(const u32x4 *)(row + k0 + i), v + i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = k0 + i < K ? T::load1(row + k0 + i) : 0.f;
+    }
+}
+
+// v = hi + mid + lo exactly, for every finite v: hi is cut off, so that it never overflows.  Infinities and NaNs have one term.
+__device__ inline void mx4_split3(float v, uint32_t &hi, uint32_t &mid, uint32_t &lo) {
+    const uint32_t u = __float_as_uint(v);
+    hi = u >> 16;
+    mid = lo = 0;
+    if ((u & 0x7f800000u) == 0x7f800000u) {
+        if (u & 0x007fffffu) hi |= 0x40u;
+        return;
+    }
+    const float r = v - __uint_as_float(hi << 16);
+    mid = f32_to_bf16_rne_finite(r);
+    lo = f32_to_bf16_rne_finite(r - __uint_as_float(mid << 16));
+}
+
+// Eight values to three units of eight bf16, a term each.
+__device__ inline void mx4_split8(const float *v, u32x4 (&t)[3]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t h[2], m[2], l[2];
+        mx4_split3(v[2 * i], h[0], m[0], l[0]);
+        mx4_split3(v[2 * i + 1], h[1], m[1], l[1]);
+        t[0][i] = pack2(h[0], h[1]);
+        t[1][i] = pack2(m[0], m[1]);
+        t[2][i] = pack2(l[0], l[1]);
+    }
 }
 
 __device__ inline float load_as_f32(const void *p, int dtype, int64_t i) {
@@ -40,24 +92,29 @@ __device__ inline bool mx4_out_by_fours(const Mx4Out &o) {
     const uintptr_t bits = o.dtype == F32 ? 15 : 7;
     return ((uintptr_t)o.y & bits) == 0 && (o.ld & 3) == 0 && (!o.residual || (((uintptr_t)o.residual & bits) == 0 && (o.ld_res & 3) == 0));
 }
-// Values [row, row + n) of row r, 0 <= n <= 4; vec: as mx4_out_by_fours says.
-__device__ inline f32x4 mx4_residual4(const Mx4Out &o, int r, int row, int n, bool vec) {
+// Residual values [row, row + n) of row r, 0 <= n <= 4, as they are loaded (vec, as mx4_out_by_fours says, and all four: the words in memory, so that nothing
+// waits for them here; else fp32), and as numbers.
+__device__ inline u32x4 mx4_residual_words(const Mx4Out &o, int r, int row, int n, bool vec) {
     const int64_t at = r * o.ld_res + row;
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    u32x4 w = {0u, 0u, 0u, 0u};
     if (vec && n == 4) {
         if (o.dtype == F32) {
-            v = *(const f32x4 *)((const float *)o.residual + at);
+            w = *(const u32x4 *)((const float *)o.residual + at);
         } else {
-            const uint64_t w = *(const uint64_t *)((const uint16_t *)o.residual + at);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = __uint_as_float((uint32_t)(w >> (16 * i)) << 16);
+            const uint2 b = *(const uint2 *)((const uint16_t *)o.residual + at);
+            w[0] = b.x;
+            w[1] = b.y;
         }
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (i < n) v[i] = load_as_f32(o.residual, o.dtype, at + i);
+            if (i < n) w[i] = __float_as_uint(load_as_f32(o.residual, o.dtype, at + i));
     }
-    return v;
+    return w;
+}
+__device__ inline f32x4 mx4_residual_values(const Mx4Out &o, const u32x4 &w, int n, bool vec) {
+    if (o.dtype == F32 || !(vec && n == 4)) return __builtin_bit_cast(f32x4, w);
+    return f32x4{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xffff0000u), __uint_as_float(w[1] << 16), __uint_as_float(w[1] & 0xffff0000u)};
 }
 __device__ inline void mx4_store4(const Mx4Out &o, int r, int row, int n, bool vec, const f32x4 &v) {
     const int64_t at = r * o.ld + row;
@@ -74,27 +131,6 @@ __device__ inline void mx4_store4(const Mx4Out &o, int r, int row, int n, bool v
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (i < n) store_f32_as(o.y, o.dtype, at + i, v[i]);
-    }
-}
-
-// What follows the dot products of one row group of a call, by thread t of `threads`.  Y(r, j): row r's product with tile row j.
-template <int EPI, typename YF>
-__device__ inline void mx4_call_epilogue(const Mx4Out &o, int R, int O, int rg, int t, int threads, YF Y) {
-    if (EPI == EPI_LINEAR) {
-        for (int i = t; i < 16 * R; i += threads) {
-            const int r = i >> 4, row = 16 * rg + (i & 15);
-            if (row >= O) continue;
-            float y = Y(r, i & 15);
-            if (o.residual) y += load_as_f32(o.residual, o.dtype, r * o.ld_res + row);
-            store_f32_as(o.y, o.dtype, r * o.ld + row, y);
-        }
-    } else {
-        for (int i = t; i < 8 * R; i += threads) {
-            const int r = i >> 3, j = i & 7, row = 8 * rg + j;
-            if (row >= O) continue;
-            const float g = Y(r, j), u = Y(r, j + 8);
-            store_f32_as(o.y, o.dtype, r * o.ld + row, mx4_silu(g) * u);
-        }
     }
 }
 

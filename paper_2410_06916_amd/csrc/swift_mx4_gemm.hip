@@ -9,8 +9,6 @@
 // super-tiles of 128 k, two deep.  One barrier a stage, with what is multiplied first behind it in registers already: a barrier costs
 // 0.15 us whatever lies between two of them, so small tiles have longer stages.  Within a stage the next column blocks' operands are
 // read while the last ones' are multiplied, and the next quarter's codes are decoded between the matrix instructions.
-#include <utility>
-
 #include "swift_gemm.h"
 #include "swift_mx4.h"
 #include "swift_mx4_device.h"
@@ -18,16 +16,6 @@
 namespace swift {
 
 namespace {
-
-// f(0), f(1), .. f(N - 1), each a constant.
-template <int N, typename F, int... I>
-__device__ inline void each_of(F &&f, std::integer_sequence<int, I...>) {
-    (f(std::integral_constant<int, I>()), ...);
-}
-template <int N, typename F>
-__device__ inline void each(F &&f) {
-    each_of<N>(f, std::make_integer_sequence<int, N>());
-}
 
 struct Mx4GemmArgs {
     Mx4Matrix w;
@@ -295,13 +283,13 @@ __global__ __launch_bounds__(512) void k_mx4_gemm(Mx4GemmArgs q) {
                 }
                 return r < rows ? min(max(a.O - row, 0), 4) : 0;
             };
-            f32x4 res[2][N];  // a row group's residual values, requested while the one before it is written
+            u32x4 res[2][N];  // a row group's residual values, requested while the one before it is written
             auto request = [&](int g) {
 #pragma unroll
                 for (int c = 0; c < N; ++c) {
                     int r, row;
                     const int n = place(g, c, r, row);
-                    res[g & 1][c] = mx4_residual4(o, r, row, n, vec);
+                    res[g & 1][c] = mx4_residual_words(o, r, row, n, vec);
                 }
             };
             if (EPI == EPI_LINEAR && o.residual) request(0);
@@ -315,7 +303,7 @@ __global__ __launch_bounds__(512) void k_mx4_gemm(Mx4GemmArgs q) {
                     f32x4 v;
                     if constexpr (EPI == EPI_LINEAR) {
                         v = acc[g][c];
-                        if (o.residual) v += res[g & 1][c];
+                        if (o.residual) v += mx4_residual_values(o, res[g & 1][c], n, vec);
                     } else {
                         f32x4 ga = acc[g][2 * c], up = acc[g][2 * c + 1];
 #pragma unroll
@@ -348,7 +336,7 @@ __global__ __launch_bounds__(512) void k_mx4_gemm(Mx4GemmArgs q) {
                     };
                     f32x4 y = sum(j);
                     if constexpr (EPI == EPI_LINEAR) {
-                        if (o.residual) y += mx4_residual4(o, r, row, n, vec);
+                        if (o.residual) y += mx4_residual_values(o, mx4_residual_words(o, r, row, n, vec), n, vec);
                     } else {
                         const f32x4 up = sum(8 + j);
 #pragma unroll

@@ -17,18 +17,6 @@ __device__ inline int tile_row(int mode, int part, int d, int rg, int j) {
     return head * d + 8 * g + (j & 7) + (j >= 8 ? d >> 1 : 0);
 }
 
-// Elements k0 .. k0 + 7 of a row as fp32, zeros past K.  vec: the row allows 16-byte loads.
-template <typename T>
-__device__ inline void load8(const typename T::elem *row, int k0, int K, bool vec, float *v) {
-    if (vec && k0 + 8 <= K) {
-#pragma unroll
-        for (int i = 0; i < 8; i += T::VEC) T::unpack(*(const u32x4 *)(row + k0 + i), v + i);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = k0 + i < K ? T::load1(row + k0 + i) : 0.f;
-    }
-}
-
 // One lane per block of 32.  The scale's exponent is that of the largest magnitude less two (its floor(log2) against the four of the largest
 // element's binade), at least -127; the conversion instruction divides by the scale, rounds to the nearest element, ties to the even
 // code, and saturates at 6, subnormals included.
@@ -47,7 +35,7 @@ __global__ __launch_bounds__(256) void k_mx4_quantize(Mx4QuantArgs a, bool vec) 
             const auto *src = (const typename T::elem *)a.src + (int64_t)row * a.ld;
             float v[32];
 #pragma unroll
-            for (int i = 0; i < 32; i += 8) load8<T>(src, k0 + i, a.K, vec, v + i);
+            for (int i = 0; i < 32; i += 8) mx4_load8<T>(src, k0 + i, a.K, vec, v + i);
             uint32_t top = 0;
 #pragma unroll
             for (int i = 0; i < 32; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);  // (NaNs above infinity above numbers)
@@ -113,20 +101,6 @@ __global__ __launch_bounds__(256) void k_mx4_dequantize(Mx4DequantArgs a, bool v
     }
 }
 
-// v = hi + mid + lo exactly, for every finite v: hi is cut off, so that it never overflows.  Infinities and NaNs have one term.
-__device__ inline void split3_any(float v, uint32_t &hi, uint32_t &mid, uint32_t &lo) {
-    const uint32_t u = __float_as_uint(v);
-    hi = u >> 16;
-    mid = lo = 0;
-    if ((u & 0x7f800000u) == 0x7f800000u) {
-        if (u & 0x007fffffu) hi |= 0x40u;
-        return;
-    }
-    const float r = v - __uint_as_float(hi << 16);
-    mid = f32_to_bf16_rne_finite(r);
-    lo = f32_to_bf16_rne_finite(r - __uint_as_float(mid << 16));
-}
-
 // A workgroup turns 64 rows (at most) of a sub-block by 16 chunks through LDS: rows are read 128 k at a time, columns are written a KB at a
 // time.  (A thread per chunk that writes where its chunk goes: 512 rows of 4096 bf16 7.5 us.)
 constexpr int kActRows = 64;
@@ -140,20 +114,13 @@ __global__ __launch_bounds__(256) void k_mx4_activations(Mx4ActArgs a, int block
     for (int i = threadIdx.x; i < 16 * rows; i += 256) {
         const int r = i >> 4, ch = i & 15;
         float v[8];
-        load8<T>((const typename T::elem *)a.x + (int64_t)(r0 + r) * a.ld, kMx4Tile * s + 8 * ch, a.K, vec, v);
+        mx4_load8<T>((const typename T::elem *)a.x + (int64_t)(r0 + r) * a.ld, kMx4Tile * s + 8 * ch, a.K, vec, v);
         u32x4 t[3];
+        if constexpr (NT == 1) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if constexpr (NT == 1) {
-                t[0][j] = (__float_as_uint(v[2 * j]) >> 16) | (__float_as_uint(v[2 * j + 1]) & 0xffff0000u);
-            } else {
-                uint32_t h[2], m[2], l[2];
-                split3_any(v[2 * j], h[0], m[0], l[0]);
-                split3_any(v[2 * j + 1], h[1], m[1], l[1]);
-                t[0][j] = pack2(h[0], h[1]);
-                t[1][j] = pack2(m[0], m[1]);
-                t[2][j] = pack2(l[0], l[1]);
-            }
+            for (int j = 0; j < 4; ++j) t[0][j] = (__float_as_uint(v[2 * j]) >> 16) | (__float_as_uint(v[2 * j + 1]) & 0xffff0000u);
+        } else {
+            mx4_split8(v, t);
         }
 #pragma unroll
         for (int j = 0; j < NT; ++j) turn[ch * P + NT * r + j] = t[j];
