@@ -1063,8 +1063,9 @@ extern "C" int swift_load_tensor(swift_ctx *x, const char *name, const void *dat
             src = x->base + x->L.stage;
         }
         if (sl.scales != 0) {
-            const Mx4QuantArgs q{src,       SWIFT_BF16,   sl.cols,          sl.rows, sl.cols, (uint8_t *)x->base + sl.off, (uint8_t *)x->base + sl.scales,
-                                 sl.n_rg,   sl.tile_mode, x->c.head_dim,    sl.part};
+            const bool up = sl.tile_mode == TILE_GATEUP && sl.part == 1;
+            const Mx4QuantArgs q{up ? nullptr : src, up ? src : nullptr, SWIFT_BF16, sl.cols, sl.cols, sl.rows, sl.cols, (uint8_t *)x->base + sl.off,
+                                 (uint8_t *)x->base + sl.scales, sl.n_rg, sl.tile_mode, x->c.head_dim};
             HIP_TRY(launch_mx4_quantize(q, x->stream));
         } else {
             TileArgs t{};

@@ -33,12 +33,12 @@ struct Mx4Matrix {
 
 // ---- packing (swift_mx4_pack.hip)
 struct Mx4QuantArgs {
-    const void *src;  // [src_rows][K], rows ld elements apart
-    int dtype;        // F32 or BF16
-    int64_t ld;
+    const void *src, *up;  // [src_rows][K], rows ld and ld_up elements apart; TILE_GATEUP: the gate and the up rows (nullptr: left as they are)
+    int dtype;             // F32 or BF16
+    int64_t ld, ld_up;
     int src_rows, K;
     uint8_t *codes, *scales;  // first row group written
-    int n_rg, mode, head_dim, part;  // as in TileArgs
+    int n_rg, mode, head_dim;  // as in TileArgs
 };
 hipError_t launch_mx4_quantize(const Mx4QuantArgs &a, hipStream_t s);
 
@@ -48,6 +48,7 @@ struct Mx4DequantArgs {
     int dtype;
     int64_t ld;
     int rows, K, mode;  // rows: of the matrix (TILE_GATEUP: of each half); TILE_PLAIN or TILE_GATEUP
+    int row0;           // set by the launcher: row of the launch's first row group
 };
 hipError_t launch_mx4_dequantize(const Mx4DequantArgs &a, hipStream_t s);
 

@@ -139,12 +139,7 @@ extern "C" int swift_mx4_quantize(void *packed, const void *w, int64_t ld_w, con
     if (((uintptr_t)packed & 255) || !aligned(w, dtype) || (up && !aligned(up, dtype)))
         return api_fail(SWIFT_EINVAL, "a pointer is not aligned to its elements (a packed matrix: to 256 bytes)");
     const Mx4Matrix m = matrix_at(packed, rows, depth, up != nullptr);
-    Mx4QuantArgs a{w, dtype, ld_w, rows, depth, (uint8_t *)m.codes, (uint8_t *)m.scales, m.n_rg, up ? TILE_GATEUP : TILE_PLAIN, 0, 0};
-    int rc = device_status(launch_mx4_quantize(a, (hipStream_t)stream), "swift_mx4_quantize");
-    if (rc || !up) return rc;
-    a.src = up;
-    a.ld = ld_up;
-    a.part = 1;
+    const Mx4QuantArgs a{w, up, dtype, ld_w, ld_up, rows, depth, (uint8_t *)m.codes, (uint8_t *)m.scales, m.n_rg, up ? TILE_GATEUP : TILE_PLAIN, 0};
     return device_status(launch_mx4_quantize(a, (hipStream_t)stream), "swift_mx4_quantize");
 }
 
@@ -155,7 +150,7 @@ extern "C" int swift_mx4_dequantize(void *w, int64_t ld_w, int dtype, const void
     if (ld_w < depth) return api_fail(SWIFT_EINVAL, "rows overlap: a leading dimension is too small");
     if (((uintptr_t)packed & 255) || !aligned(w, dtype))
         return api_fail(SWIFT_EINVAL, "a pointer is not aligned to its elements (a packed matrix: to 256 bytes)");
-    Mx4DequantArgs a{matrix_at(packed, rows, depth, gated != 0), w, dtype, ld_w, rows, depth, gated ? TILE_GATEUP : TILE_PLAIN};
+    Mx4DequantArgs a{matrix_at(packed, rows, depth, gated != 0), w, dtype, ld_w, rows, depth, gated ? TILE_GATEUP : TILE_PLAIN, 0};
     return device_status(launch_mx4_dequantize(a, (hipStream_t)stream), "swift_mx4_dequantize");
 }
 

@@ -9,63 +9,75 @@ namespace swift {
 
 namespace {
 
-// Row of the matrix in tile row j of row group rg, or -1: it comes from the other tensor (TILE_GATEUP).
-__device__ inline int tile_row(int mode, int part, int d, int rg, int j) {
+// Both ways four lanes share a block, a lane has eight elements (a word of codes), and a wavefront four rows by 128 k, so that rows are read and
+// written in pieces of 16 lanes x 16 bytes next to each other; a workgroup covers a piece (16 rows x 128 k) and walks kAhead of them, whose
+// loads go out together.  What bounds both is memory.  (A lane per block reads and writes 64 lines an instruction: the 7B gate and up pair
+// there and back 130 us.)
+constexpr int kAhead = 4;
+struct PieceLane {
+    int j, kg, w;  // tile row, block, word
+};
+__device__ inline PieceLane piece_lane() {
+    const int t = threadIdx.x;
+    return {t >> 4, (t >> 2) & 3, t & 3};
+}
+// The largest over the four lanes of a block.
+__device__ inline uint32_t block_max(uint32_t v) {
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true));  // quad_perm [1,0,3,2]
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true));  // quad_perm [2,3,0,1]
+}
+
+// Row of the matrix in tile row j of row group rg.
+__device__ inline int tile_row(int mode, int d, int rg, int j) {
     if (mode == TILE_PLAIN) return 16 * rg + j;
-    if (mode == TILE_GATEUP) return (j >= 8) == (part == 1) ? 8 * rg + (j & 7) : -1;
+    if (mode == TILE_GATEUP) return 8 * rg + (j & 7);
     const int gph = d >> 4, head = rg / gph, g = rg - head * gph;
     return head * d + 8 * g + (j & 7) + (j >= 8 ? d >> 1 : 0);
 }
 
-// One lane per block of 32.  The scale's exponent is that of the largest magnitude less two (its floor(log2) against the four of the largest
-// element's binade), at least -127; the conversion instruction divides by the scale, rounds to the nearest element, ties to the even
-// code, and saturates at 6, subnormals included.
+// The scale's exponent is that of the largest magnitude less two (its floor(log2) against the four of the largest element's binade), at least
+// -127; the conversion instruction divides by the scale, rounds to the nearest element, ties to the even code, and saturates at 6,
+// subnormals included.
 template <typename T>
 __global__ __launch_bounds__(256) void k_mx4_quantize(Mx4QuantArgs a, bool vec) {
-    const int S = mx4_tiles(a.K);
-    const int64_t n = (int64_t)a.n_rg * S * 64;
-    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < n; c += (int64_t)gridDim.x * 256) {
-        const int64_t piece = c >> 6;
-        const int lane = (int)(c & 63), rg = (int)(piece / S), s = (int)(piece - (int64_t)rg * S);
-        const int row = tile_row(a.mode, a.part, a.head_dim, rg, lane & 15), k0 = kMx4Tile * s + kMx4Block * (lane >> 4);
-        if (row < 0) continue;
-        u32x4 code = {0u, 0u, 0u, 0u};
-        uint32_t e = 0;
-        if (row < a.src_rows && k0 < a.K) {
-            const auto *src = (const typename T::elem *)a.src + (int64_t)row * a.ld;
-            float v[32];
+    const int S = mx4_tiles(a.K), rg = blockIdx.y, s0 = blockIdx.x * kAhead;
+    const PieceLane l = piece_lane();
+    const bool up = a.mode == TILE_GATEUP && l.j >= 8;
+    if (a.mode == TILE_GATEUP && !(up ? a.up : a.src)) return;  // (that half comes another time; whole blocks leave)
+    const int row = tile_row(a.mode, a.head_dim, rg, l.j), kl = kMx4Block * l.kg + 8 * l.w;
+    const auto *src = (const typename T::elem *)(up ? a.up : a.src) + (int64_t)row * (up ? a.ld_up : a.ld);
+    const int K = row < a.src_rows ? a.K : 0;  // (rows and k past the matrix: zeros)
+    float v[kAhead][8];
 #pragma unroll
-            for (int i = 0; i < 32; i += 8) mx4_load8<T>(src, k0 + i, a.K, vec, v + i);
-            uint32_t top = 0;
+    for (int i = 0; i < kAhead; ++i) mx4_load8<T>(src, kMx4Tile * (s0 + i) + kl, K, vec, v[i]);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);  // (NaNs above infinity above numbers)
-            e = top >> 23;
-            if (e != 255) {
-                e = e > 2 ? e - 2 : 0;
-                const float scale = __uint_as_float(e << 23);  // (the instructions read its exponent field only: 0 is 2^-127)
+    for (int i = 0; i < kAhead; ++i) {
+        if (s0 + i >= S) break;
+        uint32_t top = 0;
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    uint32_t q = 0;
-                    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[8 * w], v[8 * w + 1], scale, 0);
-                    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[8 * w + 2], v[8 * w + 3], scale, 1);
-                    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[8 * w + 4], v[8 * w + 5], scale, 2);
-                    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[8 * w + 6], v[8 * w + 7], scale, 3);
-                    code[w] = q;
-                }
-            }
+        for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(v[i][k]) & 0x7fffffffu);  // (NaNs above infinity above numbers)
+        uint32_t e = block_max(top) >> 23, q = 0;
+        if (e != 255) {
+            e = e > 2 ? e - 2 : 0;
+            const float scale = __uint_as_float(e << 23);  // (the instructions read its exponent field only: 0 is 2^-127)
+            q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[i][0], v[i][1], scale, 0);
+            q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[i][2], v[i][3], scale, 1);
+            q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[i][4], v[i][5], scale, 2);
+            q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[i][6], v[i][7], scale, 3);
         }
-        ((u32x4 *)a.codes)[c] = code;
-        a.scales[c] = (uint8_t)e;
+        const int64_t piece = (int64_t)rg * S + s0 + i;
+        ((uint32_t *)a.codes)[piece * 256 + (16 * l.kg + l.j) * 4 + l.w] = q;
+        if (l.w == 0) a.scales[piece * 64 + 16 * l.kg + l.j] = (uint8_t)e;
     }
 }
 
 template <typename T>
-__device__ inline void store8(typename T::elem *row, int k0, int K, bool vec, const float *v) {
+__device__ inline void store8(typename T::elem *row, int k0, int K, bool vec, const bf16x8 &b) {
+    const u32x4 w = __builtin_bit_cast(u32x4, b);  // (every value is a bf16 number, subnormal ones included: nothing is rounded)
+    float v[8];
+    BF16T::unpack(w, v);
     if (vec && k0 + 8 <= K) {
         if constexpr (T::VEC == 8) {
-            u32x4 w;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = (__float_as_uint(v[2 * i]) >> 16) | (__float_as_uint(v[2 * i + 1]) & 0xffff0000u);
             *(u32x4 *)(row + k0) = w;
         } else {
             *(f32x4 *)(row + k0) = f32x4{v[0], v[1], v[2], v[3]};
@@ -78,26 +90,24 @@ __device__ inline void store8(typename T::elem *row, int k0, int K, bool vec, co
     }
 }
 
-// Eight codes as fp32 (every value is a bf16 number, subnormal ones included: nothing is rounded on the way out).
-__device__ inline void decode8(uint32_t w, float scale, float *v) { BF16T::unpack(__builtin_bit_cast(u32x4, mx4_decode(w, scale)), v); }
-
 template <typename T>
 __global__ __launch_bounds__(256) void k_mx4_dequantize(Mx4DequantArgs a, bool vec) {
-    const int64_t n = (int64_t)a.w.n_rg * a.w.S * 64;
-    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < n; c += (int64_t)gridDim.x * 256) {
-        const int64_t piece = c >> 6;
-        const int lane = (int)(c & 63), j = lane & 15, rg = (int)(piece / a.w.S), s = (int)(piece - (int64_t)rg * a.w.S);
-        const int row = a.mode == TILE_GATEUP ? 8 * rg + (j & 7) : 16 * rg + j, k0 = kMx4Tile * s + kMx4Block * (lane >> 4);
-        if (row >= a.rows || k0 >= a.K) continue;
-        auto *dst = (typename T::elem *)a.dst + (int64_t)(a.mode == TILE_GATEUP && j >= 8 ? row + a.rows : row) * a.ld;
-        const u32x4 code = ((const u32x4 *)a.w.codes)[c];
-        const float scale = __uint_as_float((uint32_t)a.w.scales[c] << 23);
+    const int S = a.w.S, rg = blockIdx.y, s0 = blockIdx.x * kAhead;
+    const PieceLane l = piece_lane();
+    const int row = a.row0 + tile_row(a.mode, 0, rg, l.j), kl = kMx4Block * l.kg + 8 * l.w;
+    if (row >= a.rows) return;
+    auto *dst = (typename T::elem *)a.dst + (int64_t)(a.mode == TILE_GATEUP && l.j >= 8 ? row + a.rows : row) * a.ld;
+    uint32_t code[kAhead], e[kAhead];
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            float v[8];
-            decode8(code[w], scale, v);
-            store8<T>(dst, k0 + 8 * w, a.K, vec, v);
-        }
+    for (int i = 0; i < kAhead; ++i) {
+        const int64_t piece = (int64_t)rg * S + min(s0 + i, S - 1);
+        code[i] = ((const uint32_t *)a.w.codes)[piece * 256 + (16 * l.kg + l.j) * 4 + l.w];
+        e[i] = a.w.scales[piece * 64 + 16 * l.kg + l.j];
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+        if (s0 + i >= S) break;
+        store8<T>(dst, kMx4Tile * (s0 + i) + kl, a.K, vec, mx4_decode(code[i], __uint_as_float(e[i] << 23)));
     }
 }
 
@@ -133,7 +143,6 @@ __global__ __launch_bounds__(256) void k_mx4_activations(Mx4ActArgs a, int block
         for (int c = lane; c < cols; c += 64) out[(int64_t)ch * a.pitch + c] = turn[ch * P + c];
 }
 
-unsigned grid_of(int64_t n) { return (unsigned)std::min<int64_t>((n + 255) / 256, 1 << 20); }
 bool rows_of_16_bytes(const void *p, int64_t ld, int dtype) {
     const int eb = dtype == F32 ? 4 : 2;
     return ((uintptr_t)p & 15) == 0 && (ld * eb & 15) == 0;
@@ -141,24 +150,48 @@ bool rows_of_16_bytes(const void *p, int64_t ld, int dtype) {
 
 }  // namespace
 
-hipError_t launch_mx4_quantize(const Mx4QuantArgs &a, hipStream_t s) {
-    const bool vec = rows_of_16_bytes(a.src, a.ld, a.dtype);
-    const unsigned grid = grid_of((int64_t)a.n_rg * mx4_tiles(a.K) * 64);
-    if (a.dtype == F32)
-        hipLaunchKernelGGL(k_mx4_quantize<F32T>, dim3(grid), dim3(256), 0, s, a, vec);
-    else
-        hipLaunchKernelGGL(k_mx4_quantize<BF16T>, dim3(grid), dim3(256), 0, s, a, vec);
-    return hipGetLastError();
+// Row groups of one launch (the grid's second dimension).
+constexpr int kMaxRowGroups = 65535;
+
+hipError_t launch_mx4_quantize(const Mx4QuantArgs &args, hipStream_t s) {
+    const bool vec = (!args.src || rows_of_16_bytes(args.src, args.ld, args.dtype)) && (!args.up || rows_of_16_bytes(args.up, args.ld_up, args.dtype));
+    const int S = mx4_tiles(args.K), eb = args.dtype == F32 ? 4 : 2;
+    if (args.mode == TILE_PAIR && args.n_rg > kMaxRowGroups) return hipErrorInvalidValue;
+    for (int rg0 = 0; rg0 < args.n_rg; rg0 += kMaxRowGroups) {
+        Mx4QuantArgs a = args;
+        const int64_t skipped = (int64_t)rg0 * (a.mode == TILE_GATEUP ? 8 : 16);  // rows
+        if (a.src) a.src = (const char *)a.src + skipped * a.ld * eb;
+        if (a.up) a.up = (const char *)a.up + skipped * a.ld_up * eb;
+        a.src_rows -= (int)skipped;
+        a.codes += (int64_t)rg0 * S * 1024;
+        a.scales += (int64_t)rg0 * S * 64;
+        const dim3 grid((unsigned)((S + kAhead - 1) / kAhead), (unsigned)std::min(kMaxRowGroups, a.n_rg - rg0));
+        if (a.dtype == F32)
+            hipLaunchKernelGGL(k_mx4_quantize<F32T>, grid, dim3(256), 0, s, a, vec);
+        else
+            hipLaunchKernelGGL(k_mx4_quantize<BF16T>, grid, dim3(256), 0, s, a, vec);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
-hipError_t launch_mx4_dequantize(const Mx4DequantArgs &a, hipStream_t s) {
-    const bool vec = rows_of_16_bytes(a.dst, a.ld, a.dtype);
-    const unsigned grid = grid_of((int64_t)a.w.n_rg * a.w.S * 64);
-    if (a.dtype == F32)
-        hipLaunchKernelGGL(k_mx4_dequantize<F32T>, dim3(grid), dim3(256), 0, s, a, vec);
-    else
-        hipLaunchKernelGGL(k_mx4_dequantize<BF16T>, dim3(grid), dim3(256), 0, s, a, vec);
-    return hipGetLastError();
+hipError_t launch_mx4_dequantize(const Mx4DequantArgs &args, hipStream_t s) {
+    const bool vec = rows_of_16_bytes(args.dst, args.ld, args.dtype);
+    for (int rg0 = 0; rg0 < args.w.n_rg; rg0 += kMaxRowGroups) {
+        Mx4DequantArgs a = args;
+        a.w.codes += (int64_t)rg0 * a.w.S * 1024;
+        a.w.scales += (int64_t)rg0 * a.w.S * 64;
+        a.row0 = rg0 * (a.mode == TILE_GATEUP ? 8 : 16);
+        const dim3 grid((unsigned)((a.w.S + kAhead - 1) / kAhead), (unsigned)std::min(kMaxRowGroups, args.w.n_rg - rg0));
+        if (a.dtype == F32)
+            hipLaunchKernelGGL(k_mx4_dequantize<F32T>, grid, dim3(256), 0, s, a, vec);
+        else
+            hipLaunchKernelGGL(k_mx4_dequantize<BF16T>, grid, dim3(256), 0, s, a, vec);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_mx4_activations(const Mx4ActArgs &a, hipStream_t s) {
