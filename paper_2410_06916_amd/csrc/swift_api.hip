@@ -1766,7 +1766,7 @@ extern "C" int swift_debug_projection_path(const swift_model_config *cfg, int n_
         return fail(SWIFT_EINVAL, "bad argument");
     int rc = swift_check_config(cfg);
     if (rc) return rc;
-    if (cfg->dtype != SWIFT_BF16) return fail(SWIFT_EINVAL, "fp32 models have one projection kernel");
+    if (cfg->dtype != SWIFT_BF16) return fail(SWIFT_EINVAL, "only bf16 models choose between these projection kernels");
     MvArgs m{};
     if ((rc = projection_sizes(*cfg, kernel_class, m))) return rc;
     m.R = rows;
@@ -1785,7 +1785,7 @@ extern "C" int swift_debug_prompt_path(const swift_model_config *cfg, int n_cu, 
         return fail(SWIFT_EINVAL, "bad argument");
     int rc = swift_check_config(cfg);
     if (rc) return rc;
-    if (cfg->dtype != SWIFT_BF16) return fail(SWIFT_EINVAL, "fp32 models have one projection kernel");
+    if (cfg->dtype != SWIFT_BF16) return fail(SWIFT_EINVAL, "only bf16 models choose between these projection kernels");
     MvArgs m{};
     if ((rc = projection_sizes(*cfg, kernel_class, m))) return rc;
     float part;

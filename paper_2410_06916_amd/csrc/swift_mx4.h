@@ -68,6 +68,9 @@ struct Mx4ActArgs {
 };
 hipError_t launch_mx4_activations(const Mx4ActArgs &a, hipStream_t s);
 
+// Columns from one chunk to the next for a launch of few rows: whole lines of 128 bytes, where there is more than one column block to read.
+inline int mx4_pitch(int columns) { return columns <= 16 ? columns : (columns + 7) / 8 * 8; }
+
 // ---- products (swift_mx4.hip; blocked: swift_mx4_gemm.hip)
 // What follows the dot products of a call that is not part of a model's pass, beside Epilogue's.
 enum Mx4Epilogue : int {
@@ -87,7 +90,7 @@ constexpr int kMx4MaxColumns = 128;
 // A model's projection (epilogue: EPI_QKV, EPI_RESID or EPI_SWIGLU) of a block of a.R rows, as launch_mv, over the row groups [rg0, a.n_rg) of w.
 hipError_t launch_mx4_mv(int epilogue, const MvArgs &a, const Mx4Matrix &w, int rg0, int n_cu, hipStream_t s);
 // A call's product: n rows (at most kMx4MaxColumns columns) against w, O results a row (EPI_GATED: of the gate and the up half each).
-// The rows: as launch_mx4_activations lays them out (one sub-block, pitched for its own columns); or as the caller has them, bf16 (direct:
+// The rows: as launch_mx4_activations lays them out (one sub-block, pitch mx4_pitch); or as the caller has them, bf16 (direct:
 // rows of 16-byte units, mx4_rows_direct) or fp32 (x32: mx4_rows_x32), ld_x elements apart.
 struct Mx4CallArgs {
     Mx4Matrix w;

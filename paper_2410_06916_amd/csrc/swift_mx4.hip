@@ -75,7 +75,7 @@ __global__ __launch_bounds__(512) void k_mx4_mv(const uint8_t *codes, const uint
     };
     // (B is contiguous chunk by chunk: past the slice and past the depth loads read nothing)
     const uint32_t b_from = __builtin_amdgcn_readfirstlane(16 * s0 * b_chunk);
-    const uint32_t b_here = __builtin_amdgcn_readfirstlane(b_from < b_bytes ? b_bytes - b_from : 0);
+    const uint32_t b_here = __builtin_amdgcn_readfirstlane(min(b_from < b_bytes ? b_bytes - b_from : 0, 16 * nv * b_chunk));
     const __amdgpu_buffer_rsrc_t xs = __builtin_amdgcn_make_buffer_rsrc((void *)(x + b_from), 0, b_here, 0x00020000);
     uint32_t b_at[NCB];
 #pragma unroll
@@ -199,7 +199,9 @@ __global__ __launch_bounds__(512) void k_mx4_mv(const uint8_t *codes, const uint
             if (!ONE && last) set_slices(seg + 1);
             each<NA>([&](auto U) {
                 constexpr int u = decltype(U)::value;
-                const bool on = base + u < nv;  // (wavefront-uniform)
+                // (wavefront-uniform.  With B in registers a window's steps past the slice multiply zeros with zeros: behind a branch the
+                // compiler waits for more loads than it has to)
+                const bool on = (SRC == kRegisters && !ONE) || base + u < nv;
                 each<4>([&](auto T) {
                     constexpr int t = decltype(T)::value, at = 4 * u + t + NBQ;  // at: in quarters from this block's start
                     u32x4(&bb)[NCB] = B[SRC == kRegisters ? (4 * u + t) % NBQ : 0];
@@ -398,7 +400,8 @@ hipError_t launch_mx4_call(int epi, const Mx4CallArgs &c, int n_cu, hipStream_t 
     rest.out = c.out;
     rest.NT = c.terms;
     rest.K = c.w.K;
-    Mx4Columns cols{c.x, NC, (uint32_t)c.w.S * 16 * NC * 16, 16, 16u * NC};
+    const uint32_t pitch = mx4_pitch(NC);
+    Mx4Columns cols{c.x, NC, (uint32_t)c.w.S * 16 * pitch * 16, 16, 16 * pitch};
     if (c.direct) {  // the call's own bf16 rows
         cols.bytes = 2u * c.w.K;
         cols.b_col = c.n == 1 ? 16 : 0;  // (lines of their own)

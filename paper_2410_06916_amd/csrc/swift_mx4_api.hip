@@ -49,7 +49,7 @@ bool few(int n, int x_dtype) { return n * mx4_terms(x_dtype) <= kFewColumns; }
 uint64_t workspace(int depth, int n, int x_dtype) {
     const uint64_t terms = mx4_terms(x_dtype);
     if (mx4_rows_x32(x_dtype, n, depth)) return 0;
-    if (few(n, x_dtype)) return (uint64_t)mx4_tiles(depth) * kMx4Tile * 2 * terms * n;
+    if (few(n, x_dtype)) return (uint64_t)mx4_tiles(depth) * kMx4Tile * 2 * mx4_pitch((int)terms * n);
     const uint64_t k = (uint64_t)mx4_act_tiles(depth) * kMx4Tile * 2;
     const int per = 128 / (int)terms, rows = std::min(n, kBlockedRows);
     return k * 128 * ((rows + per - 1) / per);
@@ -101,7 +101,7 @@ int product(int epi, const Call &c, void *stream) {
     }
     for (int r0 = 0; r0 < c.n; r0 += kBlockedRows) {
         a.n = std::min(kBlockedRows, c.n - r0);
-        Mx4ActArgs act{(const char *)c.x + r0 * c.ld_x * xb, c.x_dtype, c.ld_x, a.n, c.depth, blocked ? mx4_act_tiles(c.depth) : a.w.S, blocked ? 128 / terms : a.n, blocked ? 128 : terms * a.n,
+        Mx4ActArgs act{(const char *)c.x + r0 * c.ld_x * xb, c.x_dtype, c.ld_x, a.n, c.depth, blocked ? mx4_act_tiles(c.depth) : a.w.S, blocked ? 128 / terms : a.n, blocked ? 128 : mx4_pitch(terms * a.n),
                        (uint16_t *)c.ws};
         if (int rc = device_status(launch_mx4_activations(act, s), "activations of an MXFP4 product")) return rc;
         a.out = Mx4Out{(char *)c.y + r0 * c.ld_y * yb, c.y_dtype, c.ld_y, c.residual ? (const char *)c.residual + r0 * c.ld_res * yb : nullptr, c.ld_res};

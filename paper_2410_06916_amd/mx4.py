@@ -11,6 +11,7 @@ unless `out` is given.  There is no gradient: the weights are frozen, and tensor
 from __future__ import annotations
 
 import ctypes as C
+import functools
 from typing import Optional
 
 import torch
@@ -24,7 +25,7 @@ _F32 = torch.float32
 class Mx4Weight:
     """A packed matrix [rows][depth] (gated: a gate and an up matrix of that size each).  `data`: the packed bytes, a uint8 tensor."""
 
-    __slots__ = ("rows", "depth", "gated", "data", "device", "_workspace")
+    __slots__ = ("rows", "depth", "gated", "data", "device", "address", "_workspace")
 
     def __init__(self, rows: int, depth: int, gated: bool, data: torch.Tensor):
         if data.dtype != torch.uint8 or data.dim() != 1 or not data.is_contiguous() or data.numel() != packed_bytes(rows, depth, gated):
@@ -33,6 +34,7 @@ class Mx4Weight:
 
     def _set(self, rows, depth, gated, data):
         self.rows, self.depth, self.gated, self.data, self.device = rows, depth, gated, data, data.device
+        self.address = data.data_ptr()
         self._workspace = {}  # bytes that a product needs, by rows and type of x
 
     def to(self, device) -> "Mx4Weight":
@@ -49,6 +51,7 @@ class Mx4Weight:
         return need
 
 
+@functools.lru_cache(maxsize=1024)
 def packed_bytes(rows: int, depth: int, gated: bool = False) -> int:
     n = C.c_uint64()
     _chk(lib().swift_mx4_bytes(rows, depth, gated, C.byref(n)), "swift_mx4_bytes")
@@ -77,11 +80,12 @@ def _check(t: torch.Tensor, what: str, device=None) -> int:
 
 def _rows_of(t: torch.Tensor, what: str) -> int:
     """Elements from one row of a matrix to the next."""
-    if t.dim() != 2:
-        raise ValueError(f"{what} must be a matrix, not of shape {tuple(t.shape)}")
-    rows, width = t.shape
+    shape = t.shape
+    if len(shape) != 2:
+        raise ValueError(f"{what} must be a matrix, not of shape {tuple(shape)}")
+    rows, width = shape
     ld, step = t.stride()
-    if width > 1 and step != 1:
+    if step != 1 and width > 1:
         raise ValueError(f"the elements of a row of {what} must be contiguous")
     if rows <= 1:
         return width
@@ -90,14 +94,23 @@ def _rows_of(t: torch.Tensor, what: str) -> int:
     return ld
 
 
+_current_device, _raw_stream = torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
+_functions = {}  # the library's, by name
+
+
 def _call(name: str, device, *args):
     """The C call with torch's current stream of `device` as its last argument, `device` being current."""
-    f = getattr(lib(), name)
-    if device.index != torch.cuda.current_device():
+    f = _functions.get(name)
+    if f is None:
+        f = _functions[name] = getattr(lib(), name)
+    index = device.index
+    if index != _current_device():
         with torch.cuda.device(device):
-            _chk(f(*args, torch._C._cuda_getCurrentRawStream(device.index)), name)
+            rc = f(*args, _raw_stream(index))
     else:
-        _chk(f(*args, torch._C._cuda_getCurrentRawStream(device.index)), name)
+        rc = f(*args, _raw_stream(index))
+    if rc:
+        _chk(rc, name)
 
 
 def mx4_quantize(w: torch.Tensor) -> Mx4Weight:
@@ -105,7 +118,7 @@ def mx4_quantize(w: torch.Tensor) -> Mx4Weight:
     dt, ld = _check(w, "w"), _rows_of(w, "w")
     rows, depth = w.shape
     m = _packed(rows, depth, False, w.device)
-    _call("swift_mx4_quantize", w.device, m.data.data_ptr(), w.data_ptr(), ld, None, 0, dt, rows, depth)
+    _call("swift_mx4_quantize", w.device, m.address, w.data_ptr(), ld, None, 0, dt, rows, depth)
     return m
 
 
@@ -116,7 +129,7 @@ def mx4_quantize_gated(gate: torch.Tensor, up: torch.Tensor) -> Mx4Weight:
         raise ValueError("gate and up must be of one type and shape")
     rows, depth = gate.shape
     m = _packed(rows, depth, True, gate.device)
-    _call("swift_mx4_quantize", gate.device, m.data.data_ptr(), gate.data_ptr(), ld, up.data_ptr(), ld_up, dt, rows, depth)
+    _call("swift_mx4_quantize", gate.device, m.address, gate.data_ptr(), ld, up.data_ptr(), ld_up, dt, rows, depth)
     return m
 
 
@@ -139,8 +152,8 @@ def _as_rows(t: torch.Tensor, shape, what: str) -> torch.Tensor:
         raise ValueError(f"the rows of {what} must lie at one distance from each other") from None
 
 
-def _output(out: Optional[torch.Tensor], shape, rows: int, width: int, dtype, device):
-    """(the result, its address, row pitch and type's code); shape: as the caller sees it, [rows, width] as a matrix."""
+def _output(out: Optional[torch.Tensor], shape, width: int, dtype, device):
+    """(the result, its address, row pitch and type's code); shape: as the caller sees it, rows of `width`."""
     if out is None:
         t = torch.empty(shape, dtype=dtype, device=device)
         return t, t.data_ptr(), width, _DTYPES[dtype]
@@ -155,21 +168,27 @@ def mx4_dequantize(w: Mx4Weight, dtype: Optional[torch.dtype] = None, out: Optio
     """The numbers w stands for, [rows, depth], or [2 * rows, depth] of a gated one (gate rows first), as float32 unless dtype or out say
     otherwise; exact in either type."""
     rows = w.rows * (2 if w.gated else 1)
-    y, ptr, ld, dt = _output(out, (rows, w.depth), rows, w.depth, _out_dtype(dtype, out, _F32), w.device)
-    _call("swift_mx4_dequantize", w.device, ptr, ld, dt, w.data.data_ptr(), w.rows, w.depth, w.gated)
+    y, ptr, ld, dt = _output(out, (rows, w.depth), w.depth, _out_dtype(dtype, out, _F32), w.device)
+    _call("swift_mx4_dequantize", w.device, ptr, ld, dt, w.address, w.rows, w.depth, w.gated)
     return y
 
 
 def _activations(x: torch.Tensor, w: Mx4Weight):
-    """(x's rows as a matrix, their number, pitch, type's code, and the workspace that a product with them needs, its address and size)."""
-    dt = _check(x, "x", w.device)
-    if x.dim() < 1 or x.shape[-1] != w.depth:
-        raise ValueError(f"x must be [..., {w.depth}], not {tuple(x.shape)}")
-    m = x if x.dim() == 2 else x.reshape(-1, w.depth)
-    n = m.shape[0]
+    """(x's rows as a matrix, their number, pitch, type's code, the result's shape, the workspace that a product needs, its address and size)."""
+    dt, shape = _check(x, "x", w.device), x.shape
+    if not shape or shape[-1] != w.depth:
+        raise ValueError(f"x must be [..., {w.depth}], not {tuple(shape)}")
+    if len(shape) == 2:
+        m, n = x, shape[0]
+        y_shape = (n, w.rows)
+    else:
+        m = x.reshape(-1, w.depth)
+        n, y_shape = m.shape[0], (*shape[:-1], w.rows)
     need = w.workspace_bytes(n, dt)
-    ws = torch.empty(need, dtype=torch.uint8, device=w.device) if need else None
-    return m, n, _rows_of(m, "x"), dt, ws, ws.data_ptr() if need else None, need
+    if not need:
+        return m, n, _rows_of(m, "x"), dt, y_shape, None, None, 0
+    ws = torch.empty(need, dtype=torch.uint8, device=w.device)
+    return m, n, _rows_of(m, "x"), dt, y_shape, ws, ws.data_ptr(), need
 
 
 def mx4_linear(x: torch.Tensor, w: Mx4Weight, residual: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
@@ -178,10 +197,9 @@ def mx4_linear(x: torch.Tensor, w: Mx4Weight, residual: Optional[torch.Tensor] =
     out may be the residual."""
     if w.gated:
         raise ValueError("a gated weight goes through mx4_swiglu")
-    m, n, ld_x, x_dt, ws, ws_ptr, need = _activations(x, w)
-    shape = (*x.shape[:-1], w.rows)
-    dtype = _out_dtype(out_dtype, out, x.dtype)
-    y, y_ptr, ld_y, y_dt = _output(out, shape, n, w.rows, dtype, w.device)
+    m, n, ld_x, x_dt, shape, ws, ws_ptr, need = _activations(x, w)
+    dtype = x.dtype if out_dtype is None and out is None else _out_dtype(out_dtype, out, x.dtype)
+    y, y_ptr, ld_y, y_dt = _output(out, shape, w.rows, dtype, w.device)
     r_ptr, ld_r = None, 0
     if residual is not None:
         if residual.dtype != dtype:
@@ -189,7 +207,7 @@ def mx4_linear(x: torch.Tensor, w: Mx4Weight, residual: Optional[torch.Tensor] =
         _check(residual, "residual", w.device)
         r = _as_rows(residual, shape, "residual")
         r_ptr, ld_r = r.data_ptr(), _rows_of(r, "residual")
-    _call("swift_mx4_linear", w.device, y_ptr, ld_y, y_dt, m.data_ptr(), ld_x, x_dt, n, w.data.data_ptr(), w.rows, w.depth, r_ptr, ld_r, ws_ptr, need)
+    _call("swift_mx4_linear", w.device, y_ptr, ld_y, y_dt, m.data_ptr(), ld_x, x_dt, n, w.address, w.rows, w.depth, r_ptr, ld_r, ws_ptr, need)
     return y
 
 
@@ -197,7 +215,8 @@ def mx4_swiglu(x: torch.Tensor, w: Mx4Weight, out_dtype: Optional[torch.dtype] =
     """silu(x gate^T) * (x up^T) for x [..., depth] and a gated w: [..., rows], of x's type unless out_dtype or out say otherwise."""
     if not w.gated:
         raise ValueError("mx4_swiglu takes a gated weight, as mx4_quantize_gated makes it")
-    m, n, ld_x, x_dt, ws, ws_ptr, need = _activations(x, w)
-    y, y_ptr, ld_y, y_dt = _output(out, (*x.shape[:-1], w.rows), n, w.rows, _out_dtype(out_dtype, out, x.dtype), w.device)
-    _call("swift_mx4_swiglu", w.device, y_ptr, ld_y, y_dt, m.data_ptr(), ld_x, x_dt, n, w.data.data_ptr(), w.rows, w.depth, ws_ptr, need)
+    m, n, ld_x, x_dt, shape, ws, ws_ptr, need = _activations(x, w)
+    dtype = x.dtype if out_dtype is None and out is None else _out_dtype(out_dtype, out, x.dtype)
+    y, y_ptr, ld_y, y_dt = _output(out, shape, w.rows, dtype, w.device)
+    _call("swift_mx4_swiglu", w.device, y_ptr, ld_y, y_dt, m.data_ptr(), ld_x, x_dt, n, w.address, w.rows, w.depth, ws_ptr, need)
     return y

@@ -137,6 +137,38 @@ def test_linear_against_64_bits(P, n, rows, depth, x_dtype):
     assert bool((whole[:, :3] == 777).all()) and bool((whole[:, 3 + rows:] == 777).all())
 
 
+# rows of weights on either side of one, two, three and six row groups a compute unit (256 of them), depths on either side of what a
+# wavefront's window holds (an eighth of 4, 8 and 12 super-tiles), and the column counts that go with them
+@pytest.mark.parametrize("rows", [4096, 4112, 8208, 12304, 24600])
+@pytest.mark.parametrize("depth", [520, 4104, 4736, 8456, 12680])
+def test_few_rows_against_wide_and_deep_matrices(P, rows, depth):
+    g = torch.Generator(device="cuda").manual_seed(rows + depth)
+    w = (torch.randn(rows, depth, device="cuda", generator=g) * 0.05).to(BF)
+    packed = P.mx4_quantize(w)
+    vals = P.mx4_dequantize(packed).double()   # (tested against the definition above)
+    some = torch.randint(0, rows, (7,), generator=torch.Generator().manual_seed(1)).cuda()
+    assert torch.equal(vals[some].cpu(), plain.values(w[some]))
+    for n, dt in ((1, BF), (1, FP), (3, FP), (5, FP), (9, BF), (9, FP), (16, BF), (13, FP), (20, FP), (40, BF), (30, FP), (90, BF)):
+        x = torch.randn(n, depth, device="cuda", generator=g).to(dt)
+        want, size = x.double() @ vals.t(), x.double().abs() @ vals.abs().t()
+        got = P.mx4_linear(x, packed, out_dtype=FP)
+        bound = plain.linear_bound(want, size, depth, 3 if dt == FP else 1, FP)
+        err = (got.double() - want).abs()
+        assert bool((err <= bound).all()), (n, dt, float((err / bound).max()))
+
+
+def test_a_row_does_not_depend_on_the_rows_beside_it(P):
+    """Up to 96 columns every kernel adds a row's products in the same order (three columns an fp32 row)."""
+    for rows, depth in ((300, 1160), (4400, 4736), (8300, 520)):
+        packed, gated = P.mx4_quantize(_weight(1, rows, depth)), P.mx4_quantize_gated(_weight(2, rows, depth), _weight(3, rows, depth))
+        for dt, counts in ((FP, (1, 2, 5, 6, 9, 16, 17, 22, 32)), (BF, (1, 8, 16, 17, 33, 49, 65, 96))):
+            x = _randn(4, 96, depth, dtype=dt)
+            full, fullg = P.mx4_linear(x[:counts[-1]], packed), P.mx4_swiglu(x[:counts[-1]], gated)
+            for n in counts[:-1]:
+                assert torch.equal(P.mx4_linear(x[:n], packed), full[:n]), (rows, depth, dt, n)
+                assert torch.equal(P.mx4_swiglu(x[:n], gated), fullg[:n]), (rows, depth, dt, n)
+
+
 _GLU = [(1, 1, 1), (1, 344, 1032), (2, 8, 128), (5, 17, 100), (9, 688, 256), (10, 100, 777), (16, 72, 4096), (32, 200, 640), (40, 129, 264), (64, 96, 1000),
         (70, 65, 130), (128, 40, 512), (150, 344, 136), (520, 100, 264)]
 
