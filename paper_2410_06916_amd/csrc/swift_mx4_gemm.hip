@@ -359,16 +359,19 @@ hipError_t launch_tile(Mx4GemmArgs q, hipStream_t s) {
     return hipGetLastError();
 }
 
-// The tiles, rows x columns, and what they cost: us per super-tile (measured with all compute units at work, from the difference of two
-// depths) and per workgroup beside them (start, first stages, epilogue).
+// The tiles, rows x columns, and what they cost: us per super-tile (from the differences of depths of 4096, 8192 and 16384) and per workgroup
+// beside them (start, first stages, epilogue).  The matrix instructions alone take 1.86, 0.93, 0.70 and 0.47: the smaller tiles read more
+// of LDS for each of them.  1024 x 5120 x 5120, bf16, us with each: 112, 69, 63, 97; 512 x 4096 x 4096: 83, 48, 42, 38; 2048 x 8192 x 8192: 189
+// (1456 TFLOP/s), 207, 228, 283.
 using Tile256x256 = Mx4Tile<4, 4, 8, 1, 7>;
 using Tile256x128 = Mx4Tile<4, 4, 4, 2, 5>;
+using Tile192x128 = Mx4Tile<4, 3, 4, 2, 5>;
 using Tile128x128 = Mx4Tile<2, 4, 2, 4, 3>;
 struct TileCost {
     int rows, cols;
     double tile, fixed;
 };
-constexpr TileCost kTiles[] = {{256, 256, 1.95, 13.0}, {256, 128, 1.05, 9.0}, {128, 128, 0.88, 7.0}};
+constexpr TileCost kTiles[] = {{256, 256, 1.95, 13.0}, {256, 128, 1.06, 9.0}, {192, 128, 0.86, 8.5}, {128, 128, 0.90, 5.0}};
 
 // The cheapest in rounds of one workgroup per compute unit.  tiles: those a launch can take (the narrowest is a call's only).
 int choose(const Mx4GemmArgs &q, int n_cu, int tiles) {
@@ -389,9 +392,10 @@ int choose(const Mx4GemmArgs &q, int n_cu, int tiles) {
 template <int EPI>
 hipError_t launch_chosen(const Mx4GemmArgs &q, int n_cu, hipStream_t s) {
     constexpr bool kCall = EPI == EPI_LINEAR || EPI == EPI_GATED;
-    const int c = choose(q, n_cu, kCall ? 3 : 2);
+    const int c = choose(q, n_cu, kCall ? 4 : 3);
     if constexpr (kCall)
-        if (c == 2) return launch_tile<EPI, Tile128x128>(q, s);
+        if (c == 3) return launch_tile<EPI, Tile128x128>(q, s);
+    if (c == 2) return launch_tile<EPI, Tile192x128>(q, s);
     return c == 0 ? launch_tile<EPI, Tile256x256>(q, s) : launch_tile<EPI, Tile256x128>(q, s);
 }
 

@@ -121,19 +121,25 @@ __global__ __launch_bounds__(256) void k_mx4_activations(Mx4ActArgs a, int block
     const int s = blockIdx.x, sub = blockIdx.y / blocks_of_sub, b = blockIdx.y - sub * blocks_of_sub;
     const int r0 = sub * a.per + b * kActRows, rows = min(kActRows, min(a.per - b * kActRows, a.n - r0));
     if (rows <= 0) return;
-    for (int i = threadIdx.x; i < 16 * rows; i += 256) {
-        const int r = i >> 4, ch = i & 15;
-        float v[8];
-        mx4_load8<T>((const typename T::elem *)a.x + (int64_t)(r0 + r) * a.ld, kMx4Tile * s + 8 * ch, a.K, vec, v);
+    float v[4][8];  // (all loads together)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int r = (threadIdx.x >> 4) + 16 * j, k0 = kMx4Tile * s + 8 * (threadIdx.x & 15);
+        mx4_load8<T>((const typename T::elem *)a.x + (int64_t)(r0 + r) * a.ld, k0, r < rows ? a.K : 0, vec, v[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int r = (threadIdx.x >> 4) + 16 * j, ch = threadIdx.x & 15;
+        if (r >= rows) break;
         u32x4 t[3];
         if constexpr (NT == 1) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) t[0][j] = (__float_as_uint(v[2 * j]) >> 16) | (__float_as_uint(v[2 * j + 1]) & 0xffff0000u);
+            for (int i = 0; i < 4; ++i) t[0][i] = (__float_as_uint(v[j][2 * i]) >> 16) | (__float_as_uint(v[j][2 * i + 1]) & 0xffff0000u);
         } else {
-            mx4_split8(v, t);
+            mx4_split8(v[j], t);
         }
 #pragma unroll
-        for (int j = 0; j < NT; ++j) turn[ch * P + NT * r + j] = t[j];
+        for (int i = 0; i < NT; ++i) turn[ch * P + NT * r + i] = t[i];
     }
     __syncthreads();
     const int cols = NT * rows;
