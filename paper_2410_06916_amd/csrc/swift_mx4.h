@@ -84,12 +84,13 @@ struct Mx4Out {
     const void *residual;  // nullptr, or of y's type
     int64_t ld_res;
 };
-// Rows of a launch: as many columns as eight column blocks hold.
-constexpr int kMx4MaxColumns = 128;
+// Up to this many columns a call's product goes through the kernels that read every weight once for all rows, beyond through the
+// blocked one.
+constexpr int kMx4FewColumns = 96;
 
 // A model's projection (epilogue: EPI_QKV, EPI_RESID or EPI_SWIGLU) of a block of a.R rows, as launch_mv, over the row groups [rg0, a.n_rg) of w.
 hipError_t launch_mx4_mv(int epilogue, const MvArgs &a, const Mx4Matrix &w, int rg0, int n_cu, hipStream_t s);
-// A call's product: n rows (at most kMx4MaxColumns columns) against w, O results a row (EPI_GATED: of the gate and the up half each).
+// A call's product: n rows (at most kMx4FewColumns columns) against w, O results a row (EPI_GATED: of the gate and the up half each).
 // The rows: as launch_mx4_activations lays them out (one sub-block, pitch mx4_pitch); or as the caller has them, bf16 (direct:
 // rows of 16-byte units, mx4_rows_direct) or fp32 (x32: mx4_rows_x32), ld_x elements apart.
 struct Mx4CallArgs {
@@ -113,6 +114,11 @@ inline bool mx4_rows_direct(const void *x, int dtype, int64_t ld, int n, int K) 
 // (three columns a row in one column block, and their terms in LDS)
 inline bool mx4_rows_x32(int dtype, int n, int K) { return dtype == F32 && n <= 5 && mx4_lds_bytes(K, 1, 48 * n) <= kMx4LdsMost; }
 hipError_t launch_mx4_call(int epilogue, const Mx4CallArgs &a, int n_cu, hipStream_t s);
+
+// Up to 96 columns of a wide matrix, in the same order of sums as launch_mx4_mv and launch_mx4_call (swift_mx4_narrow.hip): a model's gate and up
+// (EPI_SWIGLU, a) or a call's (a.R, a.O, a.n_rg and out).  x: NC columns 16 bytes apart, `chunks` chunks b_chunk bytes apart, NT columns a row.
+hipError_t launch_mx4_narrow(int epilogue, const Mx4Matrix &w, const MvArgs &a, const Mx4Out &out, const void *x, int NC, int NT, int chunks, uint32_t b_chunk,
+                             int n_cu, hipStream_t s);
 
 // A prompt macro block of a model, as launch_gemm, over the row groups [rg0, a.n_rg) of w.  The activations of a sub-block are
 // mx4_act_tiles(K) super-tiles, zeros past K.

@@ -97,7 +97,7 @@ __global__ __launch_bounds__(512) void k_mx4_mv(const uint8_t *codes, const uint
     if constexpr (SRC == kLds) {
         if (real > 0)
             for (int l = 0; l < q.lines; ++l)
-                for (uint32_t p = 0; p < line - 16; p += 1024)  // (the last piece runs on into the next line's place, which comes after it)
+                for (uint32_t p = 0; p < line - 16; p += 1024)  // (a line's last 16 bytes are room between columns, read by nobody)
                     if (p + lane * 16 < line) to_lds<16>(x + (size_t)l * q.line_pitch + b_from + min(p + lane * 16, real - 16), lx + 16 + l * line + p);
     }
     NormPart np;
@@ -311,7 +311,8 @@ hipError_t launch_mv_t(const Mx4Matrix &w, const Mx4Columns &c, const Mx4MvRest 
 // Up to 16 columns, B in LDS.  us, launches back to back, one bf16 row unless said otherwise:
 //  * slices of up to 4 super-tiles (depth 4096) or 8: the whole window at once, a row group a workgroup (12288 x 4096 7.2, three to a workgroup 7.6;
 //    gate/up of 11008 x 4096 10.8 / 11.4; gate/up of 13824 x 5120 15.0, rounds of two 20.1), unless a workgroup's copy of B outweighs its
-//    codes: 9 rows, 12288 x 4096 13.4 / 8.7, gate/up 25.9 / 15.5; 3 fp32 rows, 15360 x 5120 31.0, rounds of two 16.0.
+//    codes: 9 rows, 12288 x 4096 13.4 / 8.7, gate/up 25.9 / 15.5; 3 fp32 rows, 15360 x 5120 31.0, rounds of two 16.0;
+//    with copies of 40 to 56 KB (2 fp32 rows, gate/up; 6 bf16 rows, gate/up) 17.2 / 13.0 and 15.6 / 11.9.
 //  * up to 12 (11008), one row group per compute unit: the whole window, 8.0; rounds of windows of 4 9.5.
 //  * deeper: rounds of two row groups (8192 x 28672 22.8, 5.5 TB/s).
 template <int EPI, int SRC>
@@ -333,8 +334,19 @@ hipError_t launch_mv_lds(const Mx4Matrix &w, const Mx4Columns &c, const Mx4MvRes
 //    one 20.7), beyond that rounds of two that keep B (gate/up 11008: 19.6; whole windows of three 21.7);
 //  * deeper: rounds of one row group where that is one round (4096 x 11008: 19.5, of two 24), else of three, else of six (28672 x 8192 gate/up, 32
 //    bf16 rows: 72, of three 76).
+// The two kernels' times in hundredths of a microsecond a super-tile: this file's, per row group of a compute unit, grows
+// with the columns; the other's (swift_mx4_narrow.hip), per round of workgroups of 8 or 16 row groups, much less.  Up to 32 columns and 32
+// super-tiles this one streams the weights nearly as fast as memory gives them (70000x4096 4.05 TB/s) and the other is no faster.
+bool mx4_narrow_pays(int ncb, int n_rg, int n, int n_cu) {
+    if (ncb < 2 || ncb > 6 || (ncb == 2 && n <= 4)) return false;
+    const int per = (n_rg + n_cu - 1) / n_cu, rounds = (per + 15) / 16;
+    const int few = (ncb == 2 ? 8 : ncb <= 4 ? 16 : 22) * per;
+    return few > (ncb == 2 ? 95 : ncb <= 4 ? 119 : per <= 8 ? 103 : 147) * rounds;
+}
+
 template <int EPI>
 hipError_t launch_mv_e(const Mx4Matrix &w, const Mx4Columns &c, Mx4MvRest rest, int rg0, int n_cu, hipStream_t s) {
+    constexpr bool kModel = EPI == EPI_QKV || EPI == EPI_RESID || EPI == EPI_SWIGLU;
     const int ncb = (c.NC + 15) / 16, n_rg = rest.a.n_rg - rg0, n = (w.S + 7) / 8;
     if (ncb == 1) {
         rest.lines = c.b_col == 16 ? 1 : c.NC;
@@ -342,6 +354,10 @@ hipError_t launch_mv_e(const Mx4Matrix &w, const Mx4Columns &c, Mx4MvRest rest, 
         if (lds_b <= kMx4LdsMost) return launch_mv_lds<EPI, kLds>(w, c, rest, rg0, n_cu, lds_b, s);
     }
     const int per = (n_rg + n_cu - 1) / n_cu;  // row groups a compute unit
+    if constexpr (EPI == EPI_SWIGLU || !kModel) {  // (the other projections of a model do not have that many rows)
+        if (c.b_col == 16 && mx4_narrow_pays(ncb, n_rg, n, n_cu))
+            return launch_mx4_narrow(EPI, w, rest.a, rest.out, c.x, c.NC, rest.NT, (int)(c.bytes / c.b_chunk), c.b_chunk, n_cu, s);
+    }
     switch (ncb) {
         case 1:
         case 2:
@@ -364,7 +380,8 @@ hipError_t launch_mv_e(const Mx4Matrix &w, const Mx4Columns &c, Mx4MvRest rest, 
             if (per == 1) return launch_mv_t<EPI, 6, 1, 2, 4, kRegisters, false>(w, c, rest, rg0, n_cu, s);
             return launch_mv_t<EPI, 6, 2, 2, 4, kRegisters, false>(w, c, rest, rg0, n_cu, s);
         case 7:
-        case 8: return launch_mv_t<EPI, 8, 1, 2, 4, kRegisters, false>(w, c, rest, rg0, n_cu, s);
+        case 8:
+            if constexpr (kModel) return launch_mv_t<EPI, 8, 1, 2, 4, kRegisters, false>(w, c, rest, rg0, n_cu, s);
     }
     return hipErrorInvalidValue;
 }
@@ -392,7 +409,7 @@ hipError_t launch_mx4_mv(int epi, const MvArgs &a, const Mx4Matrix &w, int rg0, 
 
 hipError_t launch_mx4_call(int epi, const Mx4CallArgs &c, int n_cu, hipStream_t s) {
     const int NC = c.n * c.terms;
-    if (c.n < 1 || NC > kMx4MaxColumns) return hipErrorInvalidValue;
+    if (c.n < 1 || NC > kMx4FewColumns) return hipErrorInvalidValue;
     Mx4MvRest rest{};
     rest.a.R = c.n;
     rest.a.O = c.O;

@@ -40,12 +40,10 @@ int compute_units() {
     return n;
 }
 
-// Up to this many columns a product goes through the kernel that reads every weight once for all rows, beyond through the blocked one.
-constexpr int kFewColumns = 96;
 // Rows of a blocked launch (a multiple of both sub-block heights): bounds the workspace.
 constexpr int kBlockedRows = 128 * 42;
 
-bool few(int n, int x_dtype) { return n * mx4_terms(x_dtype) <= kFewColumns; }
+bool few(int n, int x_dtype) { return n * mx4_terms(x_dtype) <= kMx4FewColumns; }
 uint64_t workspace(int depth, int n, int x_dtype) {
     const uint64_t terms = mx4_terms(x_dtype);
     if (mx4_rows_x32(x_dtype, n, depth)) return 0;

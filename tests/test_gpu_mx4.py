@@ -157,6 +157,38 @@ def test_few_rows_against_wide_and_deep_matrices(P, rows, depth):
         assert bool((err <= bound).all()), (n, dt, float((err / bound).max()))
 
 
+# as many weight rows as make workgroups that share their columns worth while (5, 9, 11 and 14 row groups a compute unit), with depths on
+# either side of what such a workgroup has in flight, of eight slices, and of 32 super-tiles
+@pytest.mark.parametrize("rows,depth", [(18011, 40), (18011, 264), (18011, 1000), (18011, 2200), (33000, 40), (33000, 264), (33000, 1000), (33000, 2200),
+                                        (45008, 40), (45008, 264), (45008, 1000), (45008, 2200), (53300, 4136)])
+def test_many_columns_against_wide_matrices(P, rows, depth):
+    g = torch.Generator(device="cuda").manual_seed(rows + depth)
+    w = (torch.randn(rows, depth, device="cuda", generator=g) * 0.05).to(BF)
+    packed = P.mx4_quantize(w)
+    gated = P.mx4_quantize_gated(w[:rows // 2], w[rows // 2:2 * (rows // 2)])
+    vals = P.mx4_dequantize(packed).double()   # (tested against the definition above)
+    x96 = torch.randn(96, depth, device="cuda", generator=g)
+    r96 = torch.randn(96, rows, device="cuda", generator=g)
+    for dt, counts in ((BF, (96, 81, 65, 64, 50, 33, 32, 17)), (FP, (32, 27, 22, 21, 12, 11, 10, 6))):
+        terms = 3 if dt == FP else 1
+        for n in counts:
+            x = x96[:n].to(dt)
+            want, size = x.double() @ vals.t(), x.double().abs() @ vals.abs().t()
+            got = P.mx4_linear(x, packed, residual=r96[:n], out_dtype=FP)
+            with_r = want + r96[:n].double()
+            assert bool(((got.double() - with_r).abs() <= plain.linear_bound(with_r, size, depth, terms, FP)).all()), (n, dt)
+            half = rows // 2
+            a, b, sa, sb = want[:, :half], want[:, half:2 * half], size[:, :half], size[:, half:2 * half]
+            ref = (a / (1 + torch.exp(-a)) * b, a, b, sa, sb)
+            got_h = P.mx4_swiglu(x, gated, out_dtype=BF)
+            assert bool(((got_h.double() - ref[0]).abs() <= plain.swiglu_bound(*ref, depth, terms, BF)).all()), (n, dt)
+            if n == counts[0]:
+                full, full_h = got, got_h
+            assert torch.equal(got, full[:n]) and torch.equal(got_h, full_h[:n]), (n, dt)
+        one = P.mx4_linear(x96[:1].to(dt), packed, residual=r96[:1], out_dtype=FP)
+        assert torch.equal(one, full[:1]) and torch.equal(P.mx4_swiglu(x96[:1].to(dt), gated, out_dtype=BF), full_h[:1])
+
+
 def test_a_row_does_not_depend_on_the_rows_beside_it(P):
     """Up to 96 columns every kernel adds a row's products in the same order (three columns an fp32 row)."""
     for rows, depth in ((300, 1160), (4400, 4736), (8300, 520)):
@@ -440,6 +472,34 @@ def test_model_rows_equal_single_rows_bit_for_bit(P, case):
                 assert np.array_equal(clg[-1], lg[row + i]), (case, widths, row + i)
             row += len(lv)
             spine.append(int(lv[0]))
+    g.close()
+
+
+@pytest.mark.parametrize("intermediate", [9000, 18000, 22600])
+def test_model_blocks_with_a_wide_feed_forward_layer(P, oracle_lib, intermediate):
+    """Gate and up of enough rows that blocks share their columns between row groups: equal to one row at a time bit for bit, and to the
+    oracle's."""
+    shape = si.ModelShape("mx4-wide", 2, 520, 8, 4, 64, intermediate, 300, "bf16", 1e-5)
+    weights = hp.shaped_weights(shape, seed=6)
+    o, g = _pair(P, oracle_lib, shape, weights, 96, threads=8)
+    hp.lockstep_swift(o, g, si.uniform_ids(2, 20, shape.vocab), 12, np.array([0, 1, 1, 0], np.uint8), 8, 0.0, 2e-2)
+    g.close()
+    g = P.SwiftModel(dataclasses.replace(shape, dtype="mxfp4"), 96)
+    g.load_weights(weights)
+    g.prefill(si.uniform_ids(4, 12, shape.vocab))
+    n0, t0 = g.cache_len, g.pending
+    toks, rows = [t0], []
+    for _ in range(32):
+        tgt, lg = g.verify([g.pending], True)
+        g.accept()
+        toks.append(int(tgt[0]))
+        rows.append(lg[0].copy())
+    for R in (6, 10, 11, 17, 21, 22, 31, 32):
+        g.rollback(n0, t0)
+        tgt, lg = g.verify(toks[:R], True)
+        assert [int(x) for x in tgt] == toks[1:R + 1]
+        for r in range(R):
+            assert np.array_equal(lg[r], rows[r]), (R, r, np.abs(lg[r] - rows[r]).max())
     g.close()
 
 
