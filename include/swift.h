@@ -352,12 +352,13 @@ int swift_mx4_dequantize(void *w, int64_t ld_w, int dtype, const void *packed, i
 int swift_mx4_workspace(int rows, int depth, int gated, int n, int x_dtype, uint64_t *bytes);
 
 /* y [n][rows] = x [n][depth] W^T (+ residual [n][rows], of y's type; NULL: none).  Products are exact, sums fp32; y is rounded once.
- * n = 0 does nothing.  A row with an infinity or a NaN leaves the others as they are. */
+ * n = 0 does nothing.  A row with an infinity or a NaN leaves the others as they are.  Up to 32 fp32 or 96 bf16 rows, a row's result does not
+ * depend on how many rows share its call. */
 int swift_mx4_linear(void *y, int64_t ld_y, int y_dtype, const void *x, int64_t ld_x, int x_dtype, int n, const void *packed, int rows,
                      int depth, const void *residual, int64_t ld_residual, void *workspace, uint64_t workspace_bytes, void *stream);
 
 /* h [n][rows] = silu(x Wg^T) * (x Wu^T), silu(v) = v / (1 + exp(-v)), of a gated packed matrix: the first half of a gated feed-forward
- * block in one product. */
+ * block in one product.  Rows are independent as in swift_mx4_linear. */
 int swift_mx4_swiglu(void *h, int64_t ld_h, int h_dtype, const void *x, int64_t ld_x, int x_dtype, int n, const void *packed, int rows,
                      int depth, void *workspace, uint64_t workspace_bytes, void *stream);
 
@@ -410,7 +411,8 @@ int swift_debug_tune(swift_ctx *ctx, int kernel_class, int waves_per_row_group, 
  * library's tolerance, not the same bits).  sub_blocks: 0 = the default (macro blocks of up to 16 sub-blocks of 64
  * rows per sweep over the weights), 1..8 = macro blocks of at most that many sub-blocks, -1 = one 64-row block per
  * sweep.  tiling: 0 = automatic, else the workgroup tile of the blocked matrix product: 1..4 = 64, 128, 192 or 256
- * weight rows x two sub-blocks, 5 / 6 = 128 / 256 weight rows x one sub-block. */
+ * weight rows x two sub-blocks, 5 / 6 = 128 / 256 weight rows x one sub-block (SWIFT_MXFP4 models choose
+ * their own). */
 int swift_debug_prefill(swift_ctx *ctx, int sub_blocks, int tiling);
 
 /* Turns per-launch timing of one kernel class on (kernel_class in [0, SWIFT_KC_COUNT)) or off (-1).

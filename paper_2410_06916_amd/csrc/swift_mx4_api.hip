@@ -43,7 +43,7 @@ int compute_units() {
 // Rows of a blocked launch (a multiple of both sub-block heights): bounds the workspace.
 constexpr int kBlockedRows = 128 * 42;
 
-bool few(int n, int x_dtype) { return n * mx4_terms(x_dtype) <= kMx4FewColumns; }
+bool few(int n, int x_dtype) { return n <= kMx4FewColumns / mx4_terms(x_dtype); }
 uint64_t workspace(int depth, int n, int x_dtype) {
     const uint64_t terms = mx4_terms(x_dtype);
     if (mx4_rows_x32(x_dtype, n, depth)) return 0;
@@ -97,10 +97,11 @@ int product(int epi, const Call &c, void *stream) {
         a.out = Mx4Out{c.y, c.y_dtype, c.ld_y, c.residual, c.ld_res};
         return device_status(launch_mx4_call(epi, a, compute_units(), s), "MXFP4 product");
     }
-    for (int r0 = 0; r0 < c.n; r0 += kBlockedRows) {
-        a.n = std::min(kBlockedRows, c.n - r0);
-        Mx4ActArgs act{(const char *)c.x + r0 * c.ld_x * xb, c.x_dtype, c.ld_x, a.n, c.depth, blocked ? mx4_act_tiles(c.depth) : a.w.S, blocked ? 128 / terms : a.n, blocked ? 128 : mx4_pitch(terms * a.n),
-                       (uint16_t *)c.ws};
+    for (int64_t r0 = 0; r0 < c.n; r0 += kBlockedRows) {
+        a.n = (int)std::min<int64_t>(kBlockedRows, c.n - r0);
+        const char *x = (const char *)c.x + r0 * c.ld_x * xb;
+        const Mx4ActArgs act = blocked ? Mx4ActArgs{x, c.x_dtype, c.ld_x, a.n, c.depth, mx4_act_tiles(c.depth), 128 / terms, 128, (uint16_t *)c.ws}
+                                       : Mx4ActArgs{x, c.x_dtype, c.ld_x, a.n, c.depth, a.w.S, a.n, mx4_pitch(terms * a.n), (uint16_t *)c.ws};
         if (int rc = device_status(launch_mx4_activations(act, s), "activations of an MXFP4 product")) return rc;
         a.out = Mx4Out{(char *)c.y + r0 * c.ld_y * yb, c.y_dtype, c.ld_y, c.residual ? (const char *)c.residual + r0 * c.ld_res * yb : nullptr, c.ld_res};
         const hipError_t e = blocked ? launch_mx4_call_blocked(epi, a, compute_units(), s) : launch_mx4_call(epi, a, compute_units(), s);

@@ -12,7 +12,7 @@ namespace {
 // Both ways four lanes share a block, a lane has eight elements (a word of codes), and a wavefront four rows by 128 k, so that rows are read and
 // written in pieces of 16 lanes x 16 bytes next to each other; a workgroup covers a piece (16 rows x 128 k) and walks kAhead of them, whose
 // loads go out together.  What bounds both is memory.  (A lane per block reads and writes 64 lines an instruction: the 7B gate and up pair
-// there and back 130 us.)
+// there and back 130 us; so 87, 4.7 TB/s.)
 constexpr int kAhead = 4;
 struct PieceLane {
     int j, kg, w;  // tile row, block, word
@@ -112,7 +112,8 @@ __global__ __launch_bounds__(256) void k_mx4_dequantize(Mx4DequantArgs a, bool v
 }
 
 // A workgroup turns 64 rows (at most) of a sub-block by 16 chunks through LDS: rows are read 128 k at a time, columns are written a KB at a
-// time.  (A thread per chunk that writes where its chunk goes: 512 rows of 4096 bf16 7.5 us.)
+// time.  (A thread per chunk that writes where its chunk goes: 512 rows of 4096 bf16 7.5 us; so 4.2,
+// of which a launch is 1.7.)
 constexpr int kActRows = 64;
 template <typename T>
 __global__ __launch_bounds__(256) void k_mx4_activations(Mx4ActArgs a, int blocks_of_sub, bool vec) {

@@ -20,6 +20,7 @@ from .binding import BF16, F32, _chk, lib
 
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 _F32 = torch.float32
+_INT_MAX = (1 << 31) - 1  # (what lies beyond would be cut to 32 bits on its way into the library)
 
 
 class Mx4Weight:
@@ -53,6 +54,8 @@ class Mx4Weight:
 
 @functools.lru_cache(maxsize=1024)
 def packed_bytes(rows: int, depth: int, gated: bool = False) -> int:
+    if max(rows, depth) > _INT_MAX:
+        raise ValueError("a packed matrix has at most 2^22 rows and a depth of at most 2^22")
     n = C.c_uint64()
     _chk(lib().swift_mx4_bytes(rows, depth, gated, C.byref(n)), "swift_mx4_bytes")
     return n.value
@@ -152,8 +155,8 @@ def _as_rows(t: torch.Tensor, shape, what: str) -> torch.Tensor:
         raise ValueError(f"the rows of {what} must lie at one distance from each other") from None
 
 
-def _output(out: Optional[torch.Tensor], shape, width: int, dtype, device):
-    """(the result, its address, row pitch and type's code); shape: as the caller sees it, rows of `width`."""
+def _output(out: Optional[torch.Tensor], shape, width: int, dtype, device, x=None):
+    """(the result, its address, row pitch and type's code); shape: as the caller sees it, rows of `width`; x: what it is made from."""
     if out is None:
         t = torch.empty(shape, dtype=dtype, device=device)
         return t, t.data_ptr(), width, _DTYPES[dtype]
@@ -161,14 +164,19 @@ def _output(out: Optional[torch.Tensor], shape, width: int, dtype, device):
     if out.dtype != dtype:
         raise ValueError(f"out must be {dtype}, not {out.dtype}")
     m = _as_rows(out, shape, "out")
+    if x is not None and m.data_ptr() == x.data_ptr() and m.numel():
+        raise ValueError("out may not be x, whose rows are read while results are written")
     return out, m.data_ptr(), _rows_of(m, "out"), dt
 
 
 def mx4_dequantize(w: Mx4Weight, dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The numbers w stands for, [rows, depth], or [2 * rows, depth] of a gated one (gate rows first), as float32 unless dtype or out say
     otherwise; exact in either type."""
+    dtype = _out_dtype(dtype, out, _F32)
+    if not w.data.is_cuda:
+        raise ValueError("the weight must be on the GPU")
     rows = w.rows * (2 if w.gated else 1)
-    y, ptr, ld, dt = _output(out, (rows, w.depth), w.depth, _out_dtype(dtype, out, _F32), w.device)
+    y, ptr, ld, dt = _output(out, (rows, w.depth), w.depth, dtype, w.device)
     _call("swift_mx4_dequantize", w.device, ptr, ld, dt, w.address, w.rows, w.depth, w.gated)
     return y
 
@@ -184,6 +192,8 @@ def _activations(x: torch.Tensor, w: Mx4Weight):
     else:
         m = x.reshape(-1, w.depth)
         n, y_shape = m.shape[0], (*shape[:-1], w.rows)
+    if n > _INT_MAX:
+        raise ValueError("x has more than 2^31 - 1 rows")
     need = w.workspace_bytes(n, dt)
     if not need:
         return m, n, _rows_of(m, "x"), dt, y_shape, None, None, 0
@@ -194,12 +204,12 @@ def _activations(x: torch.Tensor, w: Mx4Weight):
 def mx4_linear(x: torch.Tensor, w: Mx4Weight, residual: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
                out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x [..., depth] times w transposed, plus residual [..., rows]: [..., rows], of x's type unless out_dtype or out say otherwise.
-    out may be the residual."""
+    out may be the residual, and overlaps no other tensor of the call."""
     if w.gated:
         raise ValueError("a gated weight goes through mx4_swiglu")
     m, n, ld_x, x_dt, shape, ws, ws_ptr, need = _activations(x, w)
     dtype = x.dtype if out_dtype is None and out is None else _out_dtype(out_dtype, out, x.dtype)
-    y, y_ptr, ld_y, y_dt = _output(out, shape, w.rows, dtype, w.device)
+    y, y_ptr, ld_y, y_dt = _output(out, shape, w.rows, dtype, w.device, m)
     r_ptr, ld_r = None, 0
     if residual is not None:
         if residual.dtype != dtype:
@@ -207,16 +217,19 @@ def mx4_linear(x: torch.Tensor, w: Mx4Weight, residual: Optional[torch.Tensor] =
         _check(residual, "residual", w.device)
         r = _as_rows(residual, shape, "residual")
         r_ptr, ld_r = r.data_ptr(), _rows_of(r, "residual")
+        if r_ptr == y_ptr and ld_r != ld_y and n > 1:
+            raise ValueError("out and residual overlap: their rows lie at different distances")
     _call("swift_mx4_linear", w.device, y_ptr, ld_y, y_dt, m.data_ptr(), ld_x, x_dt, n, w.address, w.rows, w.depth, r_ptr, ld_r, ws_ptr, need)
     return y
 
 
 def mx4_swiglu(x: torch.Tensor, w: Mx4Weight, out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """silu(x gate^T) * (x up^T) for x [..., depth] and a gated w: [..., rows], of x's type unless out_dtype or out say otherwise."""
+    """silu(x gate^T) * (x up^T) for x [..., depth] and a gated w: [..., rows], of x's type unless out_dtype or out say otherwise.
+    out overlaps no other tensor of the call."""
     if not w.gated:
         raise ValueError("mx4_swiglu takes a gated weight, as mx4_quantize_gated makes it")
     m, n, ld_x, x_dt, shape, ws, ws_ptr, need = _activations(x, w)
     dtype = x.dtype if out_dtype is None and out is None else _out_dtype(out_dtype, out, x.dtype)
-    y, y_ptr, ld_y, y_dt = _output(out, shape, w.rows, dtype, w.device)
+    y, y_ptr, ld_y, y_dt = _output(out, shape, w.rows, dtype, w.device, m)
     _call("swift_mx4_swiglu", w.device, y_ptr, ld_y, y_dt, m.data_ptr(), ld_x, x_dt, n, w.address, w.rows, w.depth, ws_ptr, need)
     return y

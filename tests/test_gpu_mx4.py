@@ -319,6 +319,73 @@ def test_refusals_on_device(P):
         P.mx4_dequantize(w, out=torch.empty(47, 160, device="cuda"))
 
 
+def test_overlaps_and_row_counts_that_are_refused(P):
+    w = P.mx4_quantize(_weight(1, 64, 64))
+    x = _randn(2, 4, 64)
+    with pytest.raises(ValueError):
+        P.mx4_linear(x, w, out=x)
+    with pytest.raises(ValueError):
+        P.mx4_swiglu(x, P.mx4_quantize_gated(_weight(1, 64, 64), _weight(2, 64, 64)), out=x)
+    base = _randn(3, 4, 128)
+    with pytest.raises(ValueError):
+        P.mx4_linear(x, w, residual=base.view(8, 64)[:4], out=base[:, :64])
+    thin = P.mx4_quantize(_weight(1, 16, 1))
+    with pytest.raises(ValueError):
+        P.mx4_linear(torch.zeros(1, 1, device="cuda").expand((1 << 32) + 5, 1), thin)
+    with pytest.raises(ValueError):
+        P.mx4_quantize(torch.zeros(1, 1, device="cuda").expand((1 << 32) + 5, 1))
+    host = P.mx4_quantize(_weight(1, 64, 64)).to("cpu")
+    with pytest.raises(ValueError):
+        P.mx4_dequantize(host)
+    with pytest.raises(ValueError):
+        P.mx4_linear(x, host)
+
+
+@pytest.mark.parametrize("n,pitch", [(2, (1 << 31) + 8), (9, (1 << 28) + 8), (13, (1 << 28) + 4), (40, (1 << 26) + 8), (140, (1 << 24) + 8)])
+def test_rows_whose_distances_pass_32_bits(P, n, pitch):
+    """Rows of x, results and residuals (in place) so far apart that the last lie past 2^31 elements or 2^32 bytes."""
+    rows, depth = 70, 200
+    w = P.mx4_quantize(_weight(1, rows, depth))
+    gated = P.mx4_quantize_gated(_weight(2, rows, depth), _weight(3, rows, depth))
+    memory = torch.empty((n - 1) * pitch + 512, device="cuda")
+    for dt in (FP, BF):
+        far = memory.view(dt)
+        x, y = far.as_strided((n, depth), (pitch, 1)), far.as_strided((n, rows), (pitch, 1), 256)
+        near = _randn(n, n, depth, dtype=dt)
+        r = _randn(n + 1, n, rows, dtype=dt)
+        x.copy_(near)
+        y.copy_(r)
+        assert torch.equal(P.mx4_linear(x, w, residual=y, out=y), P.mx4_linear(near, w, residual=r)), dt
+        assert torch.equal(y, P.mx4_linear(near, w, residual=r))
+        P.mx4_swiglu(x, gated, out=y)
+        assert torch.equal(y, P.mx4_swiglu(near, gated))
+
+
+def test_a_matrix_of_more_than_2_to_the_32_weights(P):
+    """Rows past 2^32 weights and past 2^32 bytes of codes: as the same rows by themselves, packed, read back and multiplied."""
+    rows, depth = 1048600, 8200
+    w = torch.empty(rows, depth, dtype=BF, device="cuda")
+    for i in range(0, rows, 1 << 17):
+        w[i:i + (1 << 17)].normal_()
+    packed = P.mx4_quantize(w)
+    assert packed.data.numel() > 1 << 32
+    at = rows - 1000
+    tail = P.mx4_quantize(w[at:])
+    back = P.mx4_dequantize(packed, out=w)
+    assert torch.equal(back[at:], P.mx4_dequantize(tail, BF))
+    del back, w
+    for n, dt in ((1, BF), (5, FP), (20, BF), (64, BF), (96, BF), (130, BF)):
+        x = _randn(n, n, depth, dtype=dt)
+        got = P.mx4_linear(x, packed)[:, at:]
+        want = P.mx4_linear(x, tail)
+        if n < 100:
+            assert torch.equal(got, want), n
+        else:  # (other tiles, the same products in other sums)
+            vals = P.mx4_dequantize(tail).double()
+            exact, size = x.double() @ vals.t(), x.double().abs() @ vals.abs().t()
+            assert bool(((got.double() - exact).abs() <= plain.linear_bound(exact, size, depth, 1, BF)).all())
+
+
 def test_a_feed_forward_block_in_a_row(P):
     """The calls as they follow one another: gate and up of a normalised row, its down projection onto the residual stream, for one
     token, a verification block and a prompt, against 64 bits on the stored bf16 values in between."""

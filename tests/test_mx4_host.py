@@ -146,3 +146,20 @@ def test_the_plain_form_of_the_format():
     w[1, 6] = float("nan")
     v = plain.values(w)
     assert v[:2, :32].isnan().all() and not v[:2, 32:].isnan().any() and not v[2:].isnan().any()
+
+
+def test_sizes_past_32_bits_are_refused_not_cut(P):
+    """2^32 + 16 would arrive in the library as 16; a great number of rows (three columns each in fp32) still asks for the blocked product's
+    workspace, which is that of 5376 rows whatever lies beyond."""
+    from paper_2410_06916_amd import mx4
+    for sides in (((1 << 32) + 16, 128), (128, (1 << 32) + 16), (1 << 31, 1)):
+        with pytest.raises(ValueError):
+            mx4.packed_bytes(*sides)
+        with pytest.raises(ValueError):
+            mx4.Mx4Weight(*sides, False, torch.zeros(1088, dtype=torch.uint8))
+    n, least = C.c_uint64(), C.c_uint64()
+    for dt in (0, 1):
+        assert P.lib().swift_mx4_workspace(16, 128, 0, 128 * 42, dt, C.byref(least)) == 0
+        for rows in (128 * 42 + 1, 715827883, 1431655766, (1 << 31) - 1):
+            assert P.lib().swift_mx4_workspace(16, 128, 0, rows, dt, C.byref(n)) == 0
+            assert n.value == least.value, (dt, rows)
