@@ -170,6 +170,7 @@ Layout make_layout(const swift_model_config &c) {
     L.hs = take(subs * L.sub_hs * 2);
     L.pss = take(subs * L.sub_pss * 4);
     L.mv_part_capacity = 8192;
+    static_assert(mx4_part_bytes(kMx4FewColumns, kMx4SlicedGroups) <= (uint64_t)kGemmPartSlots * 16 * kMaxBlockRows * 4, "slices of MXFP4 products");
     L.mv_part = take((uint64_t)std::max(L.mv_part_capacity, kGemmPartSlots) * 16 * kMaxBlockRows * 4);
     L.mv_counters = take(kMvCounters * 4);
     L.stage_bytes = bf ? std::max(std::max(V * H, F * H), std::max(Q * H, KV * H)) * eb : 0;
@@ -642,7 +643,7 @@ int forward_block_tiled(swift_ctx *x, const int32_t *tokens, int R, int pos0, co
             const auto *codes = (const uint8_t *)(const void *)m.Wt;
             const Mx4Matrix w{codes, codes + mx4_code_bytes(all, m.K), m.K, mx4_tiles(m.K), all};
             HIP_TRY(timed(x, kc, weight_bytes(c.dtype, m.O - 16 * rg0, m.K), [&] {
-                return macro ? launch_mx4_macro(epi, m, ma, w, rg0, x->n_cu, s) : launch_mx4_mv(epi, m, w, rg0, x->n_cu, s);
+                return macro ? launch_mx4_macro(epi, m, ma, w, rg0, x->n_cu, s) : launch_mx4_mv(epi, m, w, rg0, x->n_cu, x->arena_scr.mv_part, s);
             }));
         } else if (macro) {
             HIP_TRY(timed(x, kc, (uint64_t)m.O * m.K * 2, [&] { return launch_gemm(epi, m, ma, x->n_cu, x->gemm_rgw, s); }));

@@ -89,7 +89,8 @@ struct Mx4Out {
 constexpr int kMx4FewColumns = 96;
 
 // A model's projection (epilogue: EPI_QKV, EPI_RESID or EPI_SWIGLU) of a block of a.R rows, as launch_mv, over the row groups [rg0, a.n_rg) of w.
-hipError_t launch_mx4_mv(int epilogue, const MvArgs &a, const Mx4Matrix &w, int rg0, int n_cu, hipStream_t s);
+// part: mx4_part_bytes(kMx4FewColumns, kMx4SlicedGroups).
+hipError_t launch_mx4_mv(int epilogue, const MvArgs &a, const Mx4Matrix &w, int rg0, int n_cu, float *part, hipStream_t s);
 // A call's product: n rows (at most kMx4FewColumns columns) against w, O results a row (EPI_GATED: of the gate and the up half each).
 // The rows: as launch_mx4_activations lays them out (one sub-block, pitch mx4_pitch); or as the caller has them, bf16 (direct:
 // rows of 16-byte units, mx4_rows_direct) or fp32 (x32: mx4_rows_x32), ld_x elements apart.
@@ -101,6 +102,7 @@ struct Mx4CallArgs {
     bool direct;
     const float *x32;
     int64_t ld_x;
+    float *part;  // for slices (mx4_sliced)
 };
 // LDS that the eight slices of B take there: each 16 bytes of zeros and its lines (columns chunk by chunk, chunk_bytes a chunk), 16 bytes apart.
 __host__ __device__ inline uint32_t mx4_lds_line(int slice_tiles, uint32_t chunk_bytes) { return 16u * slice_tiles * chunk_bytes + 16; }
@@ -115,10 +117,21 @@ inline bool mx4_rows_direct(const void *x, int dtype, int64_t ld, int n, int K) 
 inline bool mx4_rows_x32(int dtype, int n, int K) { return dtype == F32 && n <= 5 && mx4_lds_bytes(K, 1, 48 * n) <= kMx4LdsMost; }
 hipError_t launch_mx4_call(int epilogue, const Mx4CallArgs &a, int n_cu, hipStream_t s);
 
-// Up to 96 columns of a wide matrix, in the same order of sums as launch_mx4_mv and launch_mx4_call (swift_mx4_narrow.hip): a model's gate and up
-// (EPI_SWIGLU, a) or a call's (a.R, a.O, a.n_rg and out).  x: NC columns 16 bytes apart, `chunks` chunks b_chunk bytes apart, NT columns a row.
-hipError_t launch_mx4_narrow(int epilogue, const Mx4Matrix &w, const MvArgs &a, const Mx4Out &out, const void *x, int NC, int NT, int chunks, uint32_t b_chunk,
-                             int n_cu, hipStream_t s);
+// Columns in memory for B: NC of them, from x, b_col bytes from one to the next, b_chunk from one chunk of eight k to the next, `bytes` in all.
+struct Mx4Columns {
+    const void *x;
+    int NC;
+    uint32_t bytes, b_col, b_chunk;
+};
+// Up to 96 columns (b_col 16, NT a row) in the same order of sums as launch_mx4_mv and launch_mx4_call (swift_mx4_narrow.hip).  A wide matrix:
+// a model's gate and up (EPI_SWIGLU, a) or a call's (a.R, a.O, a.n_rg and out).
+hipError_t launch_mx4_narrow(int epilogue, const Mx4Matrix &w, const MvArgs &a, const Mx4Out &out, const Mx4Columns &c, int NT, int n_cu, hipStream_t s);
+// A deep one with few rows, the slices of its depth in workgroups of their own: EPI_RESID of a model or EPI_LINEAR of a call.  part:
+// mx4_part_bytes.
+constexpr int kMx4SlicedGroups = 768;
+inline bool mx4_sliced(int NC, int n_rg, int S) { return NC > 16 && NC <= kMx4FewColumns && n_rg <= kMx4SlicedGroups && S > 64; }
+constexpr uint64_t mx4_part_bytes(int NC, int n_rg) { return (uint64_t)8 * n_rg * NC * 64; }
+hipError_t launch_mx4_slices(int epilogue, const Mx4Matrix &w, const MvArgs &a, const Mx4Out &out, const Mx4Columns &c, int NT, float *part, hipStream_t s);
 
 // A prompt macro block of a model, as launch_gemm, over the row groups [rg0, a.n_rg) of w.  The activations of a sub-block are
 // mx4_act_tiles(K) super-tiles, zeros past K.

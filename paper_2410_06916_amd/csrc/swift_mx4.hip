@@ -285,13 +285,6 @@ __global__ __launch_bounds__(512) void k_mx4_mv(const uint8_t *codes, const uint
     }
 }
 
-// Columns in memory for B: NC of them, from x, b_col bytes from one to the next, b_chunk from one chunk of eight k to the next, `bytes` in all.
-struct Mx4Columns {
-    const void *x;
-    int NC;
-    uint32_t bytes, b_col, b_chunk;
-};
-
 template <int EPI, int NCB, int RG, int NA, int NBQ, int SRC, bool ONE, bool KEEP = false>
 hipError_t launch_mv_t(const Mx4Matrix &w, const Mx4Columns &c, const Mx4MvRest &rest, int rg0, int n_cu, hipStream_t s) {
     constexpr bool kNorm = EPI == EPI_QKV || EPI == EPI_SWIGLU;
@@ -345,7 +338,7 @@ bool mx4_narrow_pays(int ncb, int n_rg, int n, int n_cu) {
 }
 
 template <int EPI>
-hipError_t launch_mv_e(const Mx4Matrix &w, const Mx4Columns &c, Mx4MvRest rest, int rg0, int n_cu, hipStream_t s) {
+hipError_t launch_mv_e(const Mx4Matrix &w, const Mx4Columns &c, Mx4MvRest rest, int rg0, int n_cu, float *part, hipStream_t s) {
     constexpr bool kModel = EPI == EPI_QKV || EPI == EPI_RESID || EPI == EPI_SWIGLU;
     const int ncb = (c.NC + 15) / 16, n_rg = rest.a.n_rg - rg0, n = (w.S + 7) / 8;
     if (ncb == 1) {
@@ -354,9 +347,11 @@ hipError_t launch_mv_e(const Mx4Matrix &w, const Mx4Columns &c, Mx4MvRest rest, 
         if (lds_b <= kMx4LdsMost) return launch_mv_lds<EPI, kLds>(w, c, rest, rg0, n_cu, lds_b, s);
     }
     const int per = (n_rg + n_cu - 1) / n_cu;  // row groups a compute unit
+    if constexpr (EPI == EPI_RESID || EPI == EPI_LINEAR) {
+        if (mx4_sliced(c.NC, n_rg, w.S)) return launch_mx4_slices(EPI, w, rest.a, rest.out, c, rest.NT, part, s);
+    }
     if constexpr (EPI == EPI_SWIGLU || !kModel) {  // (the other projections of a model do not have that many rows)
-        if (c.b_col == 16 && mx4_narrow_pays(ncb, n_rg, n, n_cu))
-            return launch_mx4_narrow(EPI, w, rest.a, rest.out, c.x, c.NC, rest.NT, (int)(c.bytes / c.b_chunk), c.b_chunk, n_cu, s);
+        if (c.b_col == 16 && mx4_narrow_pays(ncb, n_rg, n, n_cu)) return launch_mx4_narrow(EPI, w, rest.a, rest.out, c, rest.NT, n_cu, s);
     }
     switch (ncb) {
         case 1:
@@ -388,7 +383,7 @@ hipError_t launch_mv_e(const Mx4Matrix &w, const Mx4Columns &c, Mx4MvRest rest, 
 
 }  // namespace
 
-hipError_t launch_mx4_mv(int epi, const MvArgs &a, const Mx4Matrix &w, int rg0, int n_cu, hipStream_t s) {
+hipError_t launch_mx4_mv(int epi, const MvArgs &a, const Mx4Matrix &w, int rg0, int n_cu, float *part, hipStream_t s) {
     const bool bulk = (a.RL & kBulkLayout) != 0;
     const int lrows = layout_rows(a.RL), NT = block_terms(a.RL), NC = NT * lrows, ncb = (NC + 15) / 16;
     if (a.R < 1 || a.R > kMaxBlockRows || (a.rp != 16 && a.rp != 64) || a.R > a.rp || a.R > lrows ||
@@ -400,9 +395,9 @@ hipError_t launch_mx4_mv(int epi, const MvArgs &a, const Mx4Matrix &w, int rg0, 
     rest.a = a;
     rest.NT = NT;
     switch (epi) {
-        case EPI_QKV: return launch_mv_e<EPI_QKV>(w, c, rest, rg0, n_cu, s);
-        case EPI_RESID: return launch_mv_e<EPI_RESID>(w, c, rest, rg0, n_cu, s);
-        case EPI_SWIGLU: return launch_mv_e<EPI_SWIGLU>(w, c, rest, rg0, n_cu, s);
+        case EPI_QKV: return launch_mv_e<EPI_QKV>(w, c, rest, rg0, n_cu, part, s);
+        case EPI_RESID: return launch_mv_e<EPI_RESID>(w, c, rest, rg0, n_cu, part, s);
+        case EPI_SWIGLU: return launch_mv_e<EPI_SWIGLU>(w, c, rest, rg0, n_cu, part, s);
     }
     return hipErrorInvalidValue;
 }
@@ -432,8 +427,8 @@ hipError_t launch_mx4_call(int epi, const Mx4CallArgs &c, int n_cu, hipStream_t 
         if (epi == EPI_GATED) return launch_mv_lds<EPI_GATED, kLdsSplit>(c.w, cols, rest, 0, n_cu, mx4_lds_bytes(c.w.K, 1, 16 * NC), s);
         return hipErrorInvalidValue;
     }
-    if (epi == EPI_LINEAR) return launch_mv_e<EPI_LINEAR>(c.w, cols, rest, 0, n_cu, s);
-    if (epi == EPI_GATED) return launch_mv_e<EPI_GATED>(c.w, cols, rest, 0, n_cu, s);
+    if (epi == EPI_LINEAR) return launch_mv_e<EPI_LINEAR>(c.w, cols, rest, 0, n_cu, c.part, s);
+    if (epi == EPI_GATED) return launch_mv_e<EPI_GATED>(c.w, cols, rest, 0, n_cu, c.part, s);
     return hipErrorInvalidValue;
 }
 

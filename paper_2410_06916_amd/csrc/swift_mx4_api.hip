@@ -44,13 +44,22 @@ int compute_units() {
 constexpr int kBlockedRows = 128 * 42;
 
 bool few(int n, int x_dtype) { return n <= kMx4FewColumns / mx4_terms(x_dtype); }
-uint64_t workspace(int depth, int n, int x_dtype) {
+// Of a product's workspace, what the rows as columns take, and the slices' sums behind them.
+uint64_t activation_bytes(int depth, int n, int x_dtype) {
     const uint64_t terms = mx4_terms(x_dtype);
     if (mx4_rows_x32(x_dtype, n, depth)) return 0;
     if (few(n, x_dtype)) return (uint64_t)mx4_tiles(depth) * kMx4Tile * 2 * mx4_pitch((int)terms * n);
     const uint64_t k = (uint64_t)mx4_act_tiles(depth) * kMx4Tile * 2;
     const int per = 128 / (int)terms, rows = std::min(n, kBlockedRows);
     return k * 128 * ((rows + per - 1) / per);
+}
+uint64_t part_bytes(int rows, int depth, bool gated, int n, int x_dtype) {
+    if (gated || !few(n, x_dtype) || mx4_rows_x32(x_dtype, n, depth)) return 0;
+    const int NC = mx4_terms(x_dtype) * n, n_rg = row_groups(rows, false);
+    return mx4_sliced(NC, n_rg, mx4_tiles(depth)) ? mx4_part_bytes(NC, n_rg) : 0;
+}
+uint64_t workspace(int rows, int depth, bool gated, int n, int x_dtype) {
+    return activation_bytes(depth, n, x_dtype) + part_bytes(rows, depth, gated, n, x_dtype);
 }
 
 struct Call {
@@ -77,7 +86,7 @@ int product(int epi, const Call &c, void *stream) {
     if (c.ld_x < c.depth || c.ld_y < c.rows || (c.residual && c.ld_res < c.rows)) return api_fail(SWIFT_EINVAL, "rows overlap: a leading dimension is too small");
     if (!aligned(c.x, c.x_dtype) || !aligned(c.y, c.y_dtype) || (c.residual && !aligned(c.residual, c.y_dtype)) || ((uintptr_t)c.packed & 255))
         return api_fail(SWIFT_EINVAL, "a pointer is not aligned to its elements (a packed matrix: to 256 bytes)");
-    const uint64_t need = workspace(c.depth, c.n, c.x_dtype);
+    const uint64_t need = workspace(c.rows, c.depth, epi == EPI_GATED, c.n, c.x_dtype);
     if (need && (!c.ws || ((uintptr_t)c.ws & 255) || c.ws_bytes < need))
         return api_fail(SWIFT_ECAPACITY, "the workspace is missing, not aligned to 256 bytes, or smaller than swift_mx4_workspace says");
     const auto s = (hipStream_t)stream;
@@ -88,6 +97,7 @@ int product(int epi, const Call &c, void *stream) {
     a.x = (const uint16_t *)c.ws;
     a.terms = terms;
     a.O = c.rows;
+    a.part = part_bytes(c.rows, c.depth, epi == EPI_GATED, c.n, c.x_dtype) ? (float *)((char *)c.ws + activation_bytes(c.depth, c.n, c.x_dtype)) : nullptr;
     if (!blocked && (mx4_rows_x32(c.x_dtype, c.n, c.depth) || mx4_rows_direct(c.x, c.x_dtype, c.ld_x, c.n, c.depth))) {
         a.n = c.n;
         a.direct = c.x_dtype == SWIFT_BF16;
@@ -121,11 +131,10 @@ extern "C" int swift_mx4_bytes(int rows, int depth, int gated, uint64_t *bytes) 
 }
 
 extern "C" int swift_mx4_workspace(int rows, int depth, int gated, int n, int x_dtype, uint64_t *bytes) {
-    (void)gated;
     if (!bytes) return api_fail(SWIFT_EINVAL, "null output");
     if (int rc = check_matrix(rows, depth)) return rc;
     if (n < 0 || !known_dtype(x_dtype)) return api_fail(SWIFT_EINVAL, "bad argument");
-    *bytes = workspace(depth, n, x_dtype);
+    *bytes = workspace(rows, depth, gated != 0, n, x_dtype);
     return SWIFT_OK;
 }
 

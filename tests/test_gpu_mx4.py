@@ -189,6 +189,51 @@ def test_many_columns_against_wide_matrices(P, rows, depth):
         assert torch.equal(one, full[:1]) and torch.equal(P.mx4_swiglu(x96[:1].to(dt), gated, out_dtype=BF), full_h[:1])
 
 
+# more than 64 super-tiles: slices of the depth in workgroups of their own, some of them short or empty; up to 768 row groups, and one more
+@pytest.mark.parametrize("rows,depth", [(1, 8200), (40, 8200), (300, 9300), (4096, 11008), (2050, 16500), (12288, 8328), (12289, 8328)])
+def test_many_columns_against_deep_matrices(P, rows, depth):
+    g = torch.Generator(device="cuda").manual_seed(rows + depth)
+    w = (torch.randn(rows, depth, device="cuda", generator=g) * 0.05).to(BF)
+    packed = P.mx4_quantize(w)
+    vals = P.mx4_dequantize(packed).double()   # (tested against the definition above)
+    x96 = torch.randn(96, depth, device="cuda", generator=g)
+    r96 = torch.randn(96, rows, device="cuda", generator=g)
+    for dt, counts in ((BF, (96, 65, 64, 33, 32, 17, 16, 1)), (FP, (32, 22, 21, 11, 10, 6, 5, 1))):
+        for n in counts:
+            x = x96[:n].to(dt)
+            want, size = x.double() @ vals.t() + r96[:n].double(), x.double().abs() @ vals.abs().t()
+            y = torch.full((n, rows + 5), 3.0, device="cuda")
+            got = P.mx4_linear(x, packed, residual=r96[:n], out=y[:, 1:1 + rows])
+            assert bool(((got.double() - want).abs() <= plain.linear_bound(want, size, depth, 3 if dt == FP else 1, FP)).all()), (n, dt)
+            assert bool((y[:, 0] == 3).all()) and bool((y[:, 1 + rows:] == 3).all())
+            if n == counts[0]:
+                full = got.clone()
+            assert torch.equal(got, full[:n]), (n, dt)
+
+
+def test_slices_of_calls_on_several_streams_and_in_graphs(P):
+    """Two captured products whose slices meet in workspaces, replayed on two streams at once with eager ones between."""
+    w = P.mx4_quantize(_weight(1, 600, 9000))
+    xs = [_randn(i, 20, 9000) for i in range(3)]
+    want = [P.mx4_linear(x, w) for x in xs]
+    graphs, outs, streams = [], [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for i in (0, 1):
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[i]):
+            outs.append(P.mx4_linear(xs[i], w))
+    for _ in range(4):
+        for y in outs:
+            y.zero_()
+        torch.cuda.synchronize()
+        for i in (0, 1):
+            with torch.cuda.stream(streams[i]):
+                graphs[i].replay()
+        eager = P.mx4_linear(xs[2], w)
+        torch.cuda.synchronize()
+        assert torch.equal(eager, want[2]) and all(torch.equal(outs[i], want[i]) for i in (0, 1))
+
+
 def test_a_row_does_not_depend_on_the_rows_beside_it(P):
     """Up to 96 columns every kernel adds a row's products in the same order (three columns an fp32 row)."""
     for rows, depth in ((300, 1160), (4400, 4736), (8300, 520)):
@@ -542,7 +587,7 @@ def test_model_rows_equal_single_rows_bit_for_bit(P, case):
     g.close()
 
 
-@pytest.mark.parametrize("intermediate", [9000, 18000, 22600])
+@pytest.mark.parametrize("intermediate", [8456, 9000, 18000, 22600])
 def test_model_blocks_with_a_wide_feed_forward_layer(P, oracle_lib, intermediate):
     """Gate and up of enough rows that blocks share their columns between row groups: equal to one row at a time bit for bit, and to the
     oracle's."""
