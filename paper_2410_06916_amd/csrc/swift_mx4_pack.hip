@@ -9,10 +9,10 @@ namespace swift {
 
 namespace {
 
-// Both ways four lanes share a block, a lane has eight elements (a word of codes), and a wavefront four rows by 128 k, so that rows are read and
-// written in pieces of 16 lanes x 16 bytes next to each other; a workgroup covers a piece (16 rows x 128 k) and walks kAhead of them, whose
+// Both ways a wavefront has four rows by 128 k, so that rows are read and written in pieces of 16 lanes x 16 bytes next to each other (quantising,
+// four lanes share a block and a lane has eight elements, a word of codes); a workgroup covers a piece (16 rows x 128 k) and walks kAhead of them, whose
 // loads go out together.  What bounds both is memory.  (A lane per block reads and writes 64 lines an instruction: the 7B gate and up pair
-// there and back 130 us; so 87, 4.7 TB/s.)
+// there and back 130 us; so 74, 5.5 TB/s.)
 constexpr int kAhead = 4;
 struct PieceLane {
     int j, kg, w;  // tile row, block, word
@@ -71,43 +71,47 @@ __global__ __launch_bounds__(256) void k_mx4_quantize(Mx4QuantArgs a, bool vec) 
     }
 }
 
-template <typename T>
-__device__ inline void store8(typename T::elem *row, int k0, int K, bool vec, const bf16x8 &b) {
-    const u32x4 w = __builtin_bit_cast(u32x4, b);  // (every value is a bf16 number, subnormal ones included: nothing is rounded)
-    float v[8];
-    BF16T::unpack(w, v);
-    if (vec && k0 + 8 <= K) {
-        if constexpr (T::VEC == 8) {
-            *(u32x4 *)(row + k0) = w;
-        } else {
-            *(f32x4 *)(row + k0) = f32x4{v[0], v[1], v[2], v[3]};
-            *(f32x4 *)(row + k0 + 4) = f32x4{v[4], v[5], v[6], v[7]};
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (k0 + i < K) T::store1(row + k0 + i, v[i]);
-    }
-}
-
+// A lane writes 16 bytes at a time, next to its neighbours': in fp32 four elements, half a word of codes, of either half of the piece.
+// fp32, 13B down projection, us: eight elements in a row as two stores of every other 16 bytes 84; so 73; past the caches, which such results
+// do not fit, 49 (6.6 TB/s).
 template <typename T>
 __global__ __launch_bounds__(256) void k_mx4_dequantize(Mx4DequantArgs a, bool vec) {
-    const int S = a.w.S, rg = blockIdx.y, s0 = blockIdx.x * kAhead;
-    const PieceLane l = piece_lane();
-    const int row = a.row0 + tile_row(a.mode, 0, rg, l.j), kl = kMx4Block * l.kg + 8 * l.w;
+    constexpr int V = T::VEC, N = 8 / V;  // elements of a store, stores of a piece
+    const int S = a.w.S, rg = blockIdx.y, s0 = blockIdx.x * kAhead, j = threadIdx.x >> 4, l = threadIdx.x & 15;
+    const int row = a.row0 + tile_row(a.mode, 0, rg, j);
     if (row >= a.rows) return;
-    auto *dst = (typename T::elem *)a.dst + (int64_t)(a.mode == TILE_GATEUP && l.j >= 8 ? row + a.rows : row) * a.ld;
-    uint32_t code[kAhead], e[kAhead];
+    auto *dst = (typename T::elem *)a.dst + (int64_t)(a.mode == TILE_GATEUP && j >= 8 ? row + a.rows : row) * a.ld;
+    uint32_t code[kAhead][N], e[kAhead][N];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-        const int64_t piece = (int64_t)rg * S + min(s0 + i, S - 1);
-        code[i] = ((const uint32_t *)a.w.codes)[piece * 256 + (16 * l.kg + l.j) * 4 + l.w];
-        e[i] = a.w.scales[piece * 64 + 16 * l.kg + l.j];
-    }
+    for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+        for (int h = 0; h < N; ++h) {
+            const int64_t piece = (int64_t)rg * S + min(s0 + i, S - 1);
+            const int k = (16 * h + l) * V, at = 16 * (k / kMx4Block) + j;  // of the super-tile; the block's place in the piece
+            const uint8_t *c = a.w.codes + piece * 1024 + at * 16 + k % kMx4Block / 2;
+            code[i][h] = V == 8 ? *(const uint32_t *)c : *(const uint16_t *)c;
+            e[i][h] = a.w.scales[piece * 64 + at];
+        }
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
         if (s0 + i >= S) break;
-        store8<T>(dst, kMx4Tile * (s0 + i) + kl, a.K, vec, mx4_decode(code[i], __uint_as_float(e[i] << 23)));
+#pragma unroll
+        for (int h = 0; h < N; ++h) {
+            const int k = kMx4Tile * (s0 + i) + (16 * h + l) * V;
+            // (every value is a bf16 number, subnormal ones included: nothing is rounded)
+            const u32x4 y = __builtin_bit_cast(u32x4, mx4_decode(code[i][h], __uint_as_float(e[i][h] << 23)));
+            auto value = [&](int u) { return __uint_as_float(u & 1 ? y[u / 2] & 0xffff0000u : y[u / 2] << 16); };
+            if (vec && k + V <= a.K) {
+                if constexpr (V == 8)
+                    __builtin_nontemporal_store(y, (u32x4 *)(dst + k));
+                else
+                    __builtin_nontemporal_store(f32x4{value(0), value(1), value(2), value(3)}, (f32x4 *)(dst + k));
+            } else {
+#pragma unroll
+                for (int u = 0; u < V; ++u)
+                    if (k + u < a.K) T::store1(dst + k + u, value(u));
+            }
+        }
     }
 }
 
